@@ -335,6 +335,78 @@ linattn_status linattn_decode(const linattn_desc *desc,
                               float *S, float *z, void *hist,
                               void *out, void *hip_stream);
 
+/* ---- Attention whose memory per sequence is bounded ----------------------------------------------------------
+ *
+ * For decoders whose layers keep a fixed amount of memory per sequence: linear attention with a decay for each head
+ * (linattn_decay_*), in a form for prompts, one for generation / verification steps, and a gradient.  The conventions at the top of this file hold, with these differences: the descriptors carry
+ * strides for every tensor of rows, and `lens` gives every batch row a length of its own.
+ *
+ *   lens         in, optional  device int32 [B]: tokens of each batch row, clamped into 0..L; NULL = L for all.
+ *                Rows behind a sequence's end are not read into anything (they may hold NaN); the output and gradient
+ *                rows there are written as zeros.
+ */
+typedef struct {
+  int64_t b, h, t; /* element strides, multiples of 8, >= 0, t <= 2^22.  An input may repeat rows (stride 0); in
+                      tensors that are written t >= d, and b, h >= d where there is more than one.              */
+} linattn_strides;
+
+/* Linear attention with a decay for each head.  Per batch row and head, lambda = exp(log_decay[h]):
+ *
+ *   S_t   = lambda S_{t-1} + k_t v_t^T          (d x d, S_{-1} = S_in or zeros)
+ *   out_t = scale * q_t^T S_t
+ *
+ * The rows enter as they are (no feature map) and there is no normaliser.
+ *   log_decay    in  device float [H], each <= 0: what is above 0 (and NaN) is read as 0, no decay; -inf forgets
+ *                everything but the token itself.  A constant of the operator: it has no gradient. */
+typedef struct {
+  int32_t B, H;            /* batch rows, heads; B * H <= 2^20                          */
+  int32_t d;               /* head dimension: 64 or 128                                */
+  int32_t io_dtype;        /* linattn_dtype of q, k, v, out and the gradients           */
+  float scale;             /* finite                                                   */
+  int32_t reserved;        /* 0                                                        */
+  linattn_strides q, k, v, out; /* prefill; the step takes dense tensors and ignores all strides */
+  linattn_strides dout, dq, dk, dv; /* gradient (with q, k, v; out is not used there)  */
+} linattn_decay_desc;
+
+/* Bytes of device scratch of linattn_decay_prefill / linattn_decay_backward (0 if none, and for an invalid
+ * descriptor): states at the starts of the parts into which a long sequence of few heads is cut. */
+size_t linattn_decay_workspace_bytes(const linattn_decay_desc *desc, int32_t L);
+size_t linattn_decay_backward_workspace_bytes(const linattn_decay_desc *desc, int32_t L);
+
+/* All L >= 0 tokens of every (b, h).
+ *   q, k, v      in   [B,H,L,d] by strides;  out  out  [B,H,L,d] by strides
+ *   S_in         in, optional   float [B,H,d,d] dense (row = key feature), NULL = zeros
+ *   S_out        out, optional  the state after lens[b] tokens; may be S_in
+ * bf16 rows: matrix cores, fp32 accumulation; in-group weights and the state's read-out are rounded to bf16 once,
+ * and what enters the state carries sixteen significant bits.  fp32 rows: exact fp32 products. */
+linattn_status linattn_decay_prefill(const linattn_decay_desc *desc, int32_t L,
+                                     const void *q, const void *k, const void *v,
+                                     const float *log_decay, const int32_t *lens,
+                                     const float *S_in, void *out, float *S_out,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Gradient of linattn_decay_prefill for sequences that start from nothing: with dout = d loss / d out,
+ *   dq_t = scale sum_{s<=t} lambda^{t-s} (dout_t.v_s) k_s
+ *   dk_s = scale sum_{t>=s} lambda^{t-s} (dout_t.v_s) q_t
+ *   dv_s = scale sum_{t>=s} lambda^{t-s} (q_t.k_s) dout_t
+ * (written, not added to).  fp32 and bf16 rows.  No atomics: the same call gives the same bits. */
+linattn_status linattn_decay_backward(const linattn_decay_desc *desc, int32_t L,
+                                      const void *q, const void *k, const void *v,
+                                      const float *log_decay, const int32_t *lens, const void *dout,
+                                      void *dq, void *dk, void *dv,
+                                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* kk tokens (1 <= kk <= LINATTN_MAX_DRAFT) per (b, h) from a running state: a generation step (kk = 1) or the
+ * verification of kk drafts, like linattn_verify.
+ *   q, k, v, out [B,H,kk,d] dense;  S  in/out  float [B,H,d,d]
+ *   n_commit     in, optional  device int32 [B], clamped into 0..kk: the state advances over the first
+ *                n_commit[b] drafts (NULL: all; 0: bit-unchanged).  All kk outputs are produced.
+ * Arithmetic is fp32 throughout. */
+linattn_status linattn_decay_step(const linattn_decay_desc *desc, int32_t kk,
+                                  const void *q, const void *k, const void *v,
+                                  const float *log_decay, float *S, const int32_t *n_commit,
+                                  void *out, void *hip_stream);
+
 /* What happens when the kernels' own synchronisation fails.  The waves of a bf16 prefill workgroup hand each
  * other data through LDS and wait for one another with bounded polling, so that a logic error or an extreme
  * slowdown cannot hang the GPU.  A wait that gives up does not go unnoticed: from then on every output row

@@ -27,6 +27,7 @@ LINATTN_PHI_ELU1, LINATTN_PHI_RELU = 0, 1
 PHI = {"elu1": LINATTN_PHI_ELU1, "relu": LINATTN_PHI_RELU}
 MAX_CONV_K, MAX_CONV_K_PREFILL, MAX_DRAFT, MAX_TREE = 8, 63, 16, 64
 SYMBOLS = ("linattn_workspace_bytes", "linattn_prefill", "linattn_prefill_noalloc", "linattn_noalloc_scratch_bytes", "linattn_prefill_grouped", "linattn_backward_workspace_bytes", "linattn_prefill_grouped_backward", "linattn_verify", "linattn_verify_grouped", "linattn_verify_tree", "linattn_decode",
+           "linattn_decay_workspace_bytes", "linattn_decay_backward_workspace_bytes", "linattn_decay_prefill", "linattn_decay_backward", "linattn_decay_step",
            "linattn_set_wait_limit", "linattn_status_string", "linattn_version")
 
 
@@ -43,6 +44,16 @@ class Desc(ctypes.Structure):
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
                 ("d_v", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("stride_b_v", ctypes.c_int64), ("stride_h_v", ctypes.c_int64), ("stride_t_v", ctypes.c_int64)]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("t", ctypes.c_int64)]
+
+
+class DecayDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                *[(n, Strides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]]
 
 
 def load():
@@ -78,6 +89,13 @@ def load():
     lib.linattn_verify_tree.argtypes = [dp, i32] + [vp] * 10 + [vp]
     lib.linattn_decode.restype = ctypes.c_int
     lib.linattn_decode.argtypes = [dp] + [vp] * 8 + [vp]
+    dd = ctypes.POINTER(DecayDesc)
+    for f in (lib.linattn_decay_workspace_bytes, lib.linattn_decay_backward_workspace_bytes):
+        f.restype, f.argtypes = sz, [dd, i32]
+    for f, args in ((lib.linattn_decay_prefill, [dd, i32] + [vp] * 8 + [vp, sz, vp]),
+                    (lib.linattn_decay_backward, [dd, i32] + [vp] * 9 + [vp, sz, vp]),
+                    (lib.linattn_decay_step, [dd, i32] + [vp] * 7 + [vp])):
+        f.restype, f.argtypes = ctypes.c_int, args
     lib.linattn_status_string.restype = ctypes.c_char_p
     lib.linattn_status_string.argtypes = [ctypes.c_int]
     lib.linattn_version.restype = i32
@@ -168,6 +186,18 @@ def make_desc(B, H, d, conv_k, chunk=64, io_dtype=torch.bfloat16, eps=0.0, strid
                 *[int(s) for s in strides_v])
 
 
+def _ws_bytes(workspace, workspace_bytes) -> int:
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return int(workspace_bytes)
+
+
+def make_decay_desc(B, H, d, io_dtype=torch.bfloat16, scale=1.0, **strides) -> DecayDesc:
+    """strides: (b, h, t) in elements for each of q, k, v, out (prefill) and dout, dq, dk, dv (gradient) that the call takes."""
+    code = {torch.float32: LINATTN_F32, torch.bfloat16: LINATTN_BF16}[io_dtype]
+    return DecayDesc(B, H, d, code, float(scale), 0, **{n: Strides(*[int(x) for x in s]) for n, s in strides.items()})
+
+
 def linattn_set_wait_limit(spins: int) -> int:
     return int(load().linattn_set_wait_limit(int(spins)))
 
@@ -244,6 +274,32 @@ def linattn_decode(desc: Desc, q, k, v, conv_w, S, z, hist, out, stream=None) ->
     st = load().linattn_decode(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(conv_w),
                                _ptr(S), _ptr(z), _ptr(hist), _ptr(out), _stream(stream))
     _check(st, "linattn_decode")
+
+
+def linattn_decay_workspace_bytes(desc: DecayDesc, L) -> int:
+    return int(load().linattn_decay_workspace_bytes(ctypes.byref(desc), int(L)))
+
+
+def linattn_decay_backward_workspace_bytes(desc: DecayDesc, L) -> int:
+    return int(load().linattn_decay_backward_workspace_bytes(ctypes.byref(desc), int(L)))
+
+
+def linattn_decay_prefill(desc: DecayDesc, L, q, k, v, log_decay, lens, S_in, out, S_out, workspace=None, workspace_bytes=None, stream=None) -> None:
+    st = load().linattn_decay_prefill(ctypes.byref(desc), int(L), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lens), _ptr(S_in), _ptr(out),
+                                      _ptr(S_out), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+    _check(st, "linattn_decay_prefill")
+
+
+def linattn_decay_backward(desc: DecayDesc, L, q, k, v, log_decay, lens, dout, dq, dk, dv, workspace=None, workspace_bytes=None, stream=None) -> None:
+    st = load().linattn_decay_backward(ctypes.byref(desc), int(L), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lens), _ptr(dout), _ptr(dq),
+                                       _ptr(dk), _ptr(dv), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+    _check(st, "linattn_decay_backward")
+
+
+def linattn_decay_step(desc: DecayDesc, kk, q, k, v, log_decay, S, n_commit, out, stream=None) -> None:
+    st = load().linattn_decay_step(ctypes.byref(desc), int(kk), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(S), _ptr(n_commit), _ptr(out),
+                                   _stream(stream))
+    _check(st, "linattn_decay_step")
 
 
 # ---- conveniences that only allocate with torch and forward to the calls above ---------------
@@ -388,4 +444,104 @@ def decode(q, k, v, conv_w, state, eps=0.0, stream=None, phi="elu1"):
     out = torch.empty_like(v)
     S, z, h = state
     linattn_decode(desc, q, k, v, conv_w, S, z, h, out, stream)
+    return out
+
+
+# ---- attention whose memory per sequence is bounded ------------------------------------------
+def _rows(where, q, **others):
+    """Checks rows [B,heads,L,d] against q's type, device and last axis; the strides of those that lie in rows."""
+    if q.dim() != 4 or q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{where}: q must be a [B,H,L,d] tensor in fp32 or bf16")
+    for n, x in {"q": q, **others}.items():
+        if x.dim() != 4 or x.dtype != q.dtype or x.device != q.device or x.shape[3] != q.shape[3]:
+            raise ValueError(f"{where}: {n} must be a [B,heads,L,d] tensor of q's dtype and device")
+        if x.shape[3] > 1 and x.stride(3) != 1:
+            raise ValueError(f"{where}: {n} must be contiguous along d")
+
+
+def _aux(where, name, x, dtype, shape, device):
+    if x is not None and (x.dtype != dtype or tuple(x.shape) != tuple(shape) or x.device != device or not x.is_contiguous()):
+        raise ValueError(f"{where}: {name} must be a dense {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _st(x):
+    """(b, h, t) strides; of an axis that holds one row or none they mean nothing."""
+    return tuple(0 if n < 2 else s for n, s in zip(x.shape[:3], x.stride()))
+
+
+def _like(x):
+    """A tensor for rows laid out as x's are, dense where x is not (a slice, an expanded tensor)."""
+    return torch.empty_like(x)
+
+
+def _scratch(nbytes, device, stream):
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    if ws is not None and stream is not None and not isinstance(stream, int):
+        ws.record_stream(stream)
+    return ws
+
+
+def _on(device):
+    """The library works on the current device: make it the tensors'."""
+    if device.type != "cuda":
+        raise ValueError("the tensors must be on the GPU")
+    return torch.cuda.device(device)
+
+
+def decay_prefill(q, k, v, log_decay, scale=None, state=None, lens=None, want_state=True, stream=None):
+    """Linear attention with a decay for each head: out_t = scale * q_t^T S_t, S_t = exp(log_decay) S_{t-1} + k_t v_t^T.
+
+    q, k, v: [B,H,L,d] CUDA tensors, fp32 or bf16, of any strides that are contiguous along d (slices of a packed
+    projection, token-major views, broadcast heads).  log_decay: fp32 [H], each <= 0.  scale: None for d ** -0.5.
+    state: None or the fp32 [B,H,d,d] to go on from.  lens: None, or int32 [B], the tokens of each row; rows behind
+    them are ignored and their outputs are zeros.  Returns out (q's layout where q is dense in some order of its axes)
+    and the new state (None if not wanted)."""
+    _rows("decay_prefill", q, k=k, v=v)
+    B, H, L, d = q.shape
+    if k.shape != q.shape or v.shape != q.shape:
+        raise ValueError("decay_prefill: q, k and v must have one shape")
+    _aux("decay_prefill", "log_decay", log_decay, torch.float32, (H,), q.device)
+    _aux("decay_prefill", "state", state, torch.float32, (B, H, d, d), q.device)
+    _aux("decay_prefill", "lens", lens, torch.int32, (B,), q.device)
+    with _on(q.device):
+        out = _like(q)
+        S = torch.empty((B, H, d, d), dtype=torch.float32, device=q.device) if want_state else None
+        desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v), out=_st(out))
+        ws = _scratch(linattn_decay_workspace_bytes(desc, L), q.device, stream)
+        linattn_decay_prefill(desc, L, q, k, v, log_decay, lens, state, out, S, ws, None, stream)
+    return out, S
+
+
+def decay_backward(q, k, v, log_decay, dout, scale=None, lens=None, stream=None):
+    """Gradient of ``decay_prefill`` (from no state) with respect to q, k and v; dout: [B,H,L,d], any strides that are
+    contiguous along d.  Returns dq, dk, dv."""
+    _rows("decay_backward", q, k=k, v=v, dout=dout)
+    B, H, L, d = q.shape
+    if k.shape != q.shape or v.shape != q.shape or dout.shape != q.shape:
+        raise ValueError("decay_backward: q, k, v and dout must have one shape")
+    _aux("decay_backward", "log_decay", log_decay, torch.float32, (H,), q.device)
+    _aux("decay_backward", "lens", lens, torch.int32, (B,), q.device)
+    with _on(q.device):
+        dq, dk, dv = _like(q), _like(k), _like(v)
+        desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v),
+                               dout=_st(dout), dq=_st(dq), dk=_st(dk), dv=_st(dv))
+        ws = _scratch(linattn_decay_backward_workspace_bytes(desc, L), q.device, stream)
+        linattn_decay_backward(desc, L, q, k, v, log_decay, lens, dout, dq, dk, dv, ws, None, stream)
+    return dq, dk, dv
+
+
+def decay_step(q, k, v, log_decay, state, scale=None, n_commit=None, stream=None):
+    """kk tokens (1..16) from a running state: q, k, v dense [B,H,kk,d]; ``state`` (fp32 [B,H,d,d]) advances in place over
+    the first n_commit[b] (int32 [B]; None: all) of them.  Returns out."""
+    _rows("decay_step", q, k=k, v=v)
+    B, H, kk, d = q.shape
+    if k.shape != q.shape or v.shape != q.shape or not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+        raise ValueError("decay_step: q, k and v must be dense and of one shape")
+    _aux("decay_step", "log_decay", log_decay, torch.float32, (H,), q.device)
+    _aux("decay_step", "state", state, torch.float32, (B, H, d, d), q.device)
+    _aux("decay_step", "n_commit", n_commit, torch.int32, (B,), q.device)
+    with _on(q.device):
+        out = torch.empty_like(q)
+        desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale)
+        linattn_decay_step(desc, kk, q, k, v, log_decay, state, n_commit, out, stream)
     return out

@@ -1,0 +1,67 @@
+// Linear attention with a decay for each head: launch interfaces between the C-ABI layer (decay_api.hip) and the
+// kernels, and what the kernels share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace linattn {
+
+struct Rows {              // rows [B,H,L,d] of a tensor, addressed by element strides
+  const void* p;
+  int64_t b, h, t;
+};
+
+// out_t = scale sum_{s<=t} lambda^{t-s} (q_t . k_s) v_s, or with `reverse` the same over s >= t.  The gradient is three
+// of these with the roles of the tensors changed, so a launch carries up to three.
+struct DecayRole {
+  Rows q, k, v, out;
+  int reverse;
+};
+struct DecayArgs {
+  DecayRole role[3];
+  int roles;
+  const float* log_decay;  // [H]
+  const int32_t* lens;     // [B] or null
+  const float* S_in;       // [B,H,d,d] or null (one role only)
+  float* S_out;            // or null
+  float* ws;               // nseg > 1: [B*H][roles][nseg][d*d], the state before every segment
+  int B, H, L;
+  int nseg, seg_len;       // segments of seg_len tokens (a multiple of 64), in the order of the walk
+  float scale;
+  int exact_state;         // what enters the state carries sixteen significant bits (else eight: the gradient's own states)
+};
+hipError_t launch_decay_first_pass_bf16(const DecayArgs& a, int d, hipStream_t s);
+hipError_t launch_decay_rows_bf16(const DecayArgs& a, int d, hipStream_t s);
+hipError_t launch_decay_first_pass_f32(const DecayArgs& a, int d, hipStream_t s);
+hipError_t launch_decay_rows_f32(const DecayArgs& a, int d, hipStream_t s);
+
+struct DecayStepArgs {
+  const void *q, *k, *v;   // [B,H,kk,d] dense
+  const float* log_decay;
+  float* S;                // [B,H,d,d] in/out
+  const int32_t* n_commit;
+  void* out;
+  int B, H, kk;
+  float scale;
+};
+hipError_t launch_decay_step(const DecayStepArgs& a, int d, bool bf16, hipStream_t s);
+
+// log2 lambda of a head: log_decay <= 0, what is above 0 and NaN read as 0.  The lower bound keeps the products with a
+// count of tokens finite (and 0 * it at 0, where -inf would give NaN); 2 to any of them but 0 is 0 all the same.
+__device__ __forceinline__ float decay_log2(const float* log_decay, int h) {
+  const float g = log_decay[h] * 1.44269504088896340736f;
+  return g < 0.f ? fmaxf(g, -1e30f) : 0.f;
+}
+// lambda^n, n >= 0
+__device__ __forceinline__ float decay_pow(float g2, int n) { return __builtin_amdgcn_exp2f(g2 * (float)n); }
+
+// Which row the walk's step i is: behind the end of a sequence the rows in their own order (they are only zeroed).
+__device__ __forceinline__ int walk_row(int i, int len, int reverse) { return reverse && i < len ? len - 1 - i : i; }
+__device__ __forceinline__ int clamp_len(const int32_t* lens, int b, int L) {
+  if (!lens) return L;
+  const int n = lens[b];
+  return n < 0 ? 0 : n > L ? L : n;
+}
+
+}  // namespace linattn
