@@ -337,8 +337,9 @@ linattn_status linattn_decode(const linattn_desc *desc,
 
 /* ---- Attention whose memory per sequence is bounded ----------------------------------------------------------
  *
- * For decoders whose layers keep a fixed amount of memory per sequence: linear attention with a decay for each head
- * (linattn_decay_*), in a form for prompts, one for generation / verification steps, and a gradient.  The conventions at the top of this file hold, with these differences: the descriptors carry
+ * Two operators for decoders whose layers keep a fixed amount of memory per sequence: linear attention with a decay for
+ * each head (linattn_decay_*) and softmax attention over a sliding window with a few first tokens that stay visible
+ * (linattn_window_*).  Each has a form for prompts, one for generation / verification steps, and a gradient.  The conventions at the top of this file hold, with these differences: the descriptors carry
  * strides for every tensor of rows, and `lens` gives every batch row a length of its own.
  *
  *   lens         in, optional  device int32 [B]: tokens of each batch row, clamped into 0..L; NULL = L for all.
@@ -355,7 +356,8 @@ typedef struct {
  *   S_t   = lambda S_{t-1} + k_t v_t^T          (d x d, S_{-1} = S_in or zeros)
  *   out_t = scale * q_t^T S_t
  *
- * The rows enter as they are (no feature map) and there is no normaliser.
+ * The rows enter as they are (no feature map) and there is no normaliser.  A non-finite value in a row of a sequence may
+ * also reach earlier rows of the same 64 tokens of that sequence (never another sequence's).
  *   log_decay    in  device float [H], each <= 0: what is above 0 (and NaN) is read as 0, no decay; -inf forgets
  *                everything but the token itself.  A constant of the operator: it has no gradient. */
 typedef struct {
@@ -406,6 +408,64 @@ linattn_status linattn_decay_step(const linattn_decay_desc *desc, int32_t kk,
                                   const void *q, const void *k, const void *v,
                                   const float *log_decay, float *S, const int32_t *n_commit,
                                   void *out, void *hip_stream);
+
+/* Softmax attention over a sliding window with sinks, and shared key/value heads.  Token t of a sequence sees token s
+ * where s <= t and (s > t - window or s < sinks); query head h uses key/value head h / (H / H_kv):
+ *
+ *   out_t = sum_s softmax_s(scale * q_t.k_s) v_s,   lse_t = log sum_s exp(scale * q_t.k_s)
+ *
+ * A non-finite value in a key or value row of a sequence may also reach rows of the same sequence that do not see
+ * it (never those of another sequence). */
+typedef struct {
+  int32_t B, H, H_kv;      /* batch rows, query heads, key/value heads (a divisor of H); B * H <= 2^20 */
+  int32_t d;               /* head dimension: 64 or 128                                */
+  int32_t io_dtype;        /* linattn_dtype of q, k, v, out, the cache and the gradients */
+  int32_t window;          /* >= 1, the token itself among them                        */
+  int32_t sinks;           /* 0..LINATTN_MAX_SINKS first tokens that stay visible       */
+  float scale;             /* finite, >= 0                                             */
+  linattn_strides q, k, v, out; /* prefill (k, v: h counts key/value heads)             */
+  linattn_strides dout, dq, dk, dv; /* gradient (with q, k, v, out)                    */
+} linattn_window_desc;
+
+#define LINATTN_MAX_SINKS 64
+
+/* All L >= 0 tokens of every (b, h), from the start of the sequences.
+ *   q [B,H,L,d], k, v [B,H_kv,L,d], out [B,H,L,d]  by strides
+ *   lse          out, optional  float [B,H,L] dense; -inf behind a sequence's end
+ *   kcache, vcache  out, optional (all three or none)  [B,H_kv,sinks+window,d] dense, i/o dtype: the rows that later
+ *                tokens can see: token s < sinks in row s, any other in row sinks + (s - sinks) % window.  Rows that
+ *                no token has reached are left as they were.
+ *   pos          out, with the cache  device int32 [B,H_kv]: lens[b] */
+linattn_status linattn_window_prefill(const linattn_window_desc *desc, int32_t L,
+                                      const void *q, const void *k, const void *v, const int32_t *lens,
+                                      void *out, float *lse, void *kcache, void *vcache, int32_t *pos,
+                                      void *hip_stream);
+
+/* Gradient of linattn_window_prefill's out with respect to q, k, v (written, not added to; a key/value head's is the
+ * sum over the query heads that share it).  bf16 rows (LINATTN_ERR_UNSUPPORTED otherwise).
+ *   out, lse     in   what linattn_window_prefill gave for these inputs;  dout  in  d loss / d out
+ * Weights and their gradients are rounded to bf16 once for the products, accumulation is fp32.  No atomics. */
+size_t linattn_window_backward_workspace_bytes(const linattn_window_desc *desc, int32_t L);
+linattn_status linattn_window_backward(const linattn_window_desc *desc, int32_t L,
+                                       const void *q, const void *k, const void *v, const int32_t *lens,
+                                       const void *out, const float *lse, const void *dout,
+                                       void *dq, void *dk, void *dv,
+                                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* kk tokens (1 <= kk <= LINATTN_MAX_DRAFT) per (b, h) behind the pos tokens that the cache remembers: a generation
+ * step (kk = 1) or the verification of kk drafts.
+ *   q, out [B,H,kk,d], k, v [B,H_kv,kk,d]  dense (the descriptor's strides are ignored)
+ *   kcache, vcache, pos  in/out  as linattn_window_prefill leaves them; a new sequence has pos = 0 (the rows need not
+ *                be set).  The heads of a batch row carry equal counts, one per head so that each is read and
+ *                advanced by one owner; a negative count is read as 0, and pos + kk must stay below 2^31.
+ *   n_commit     in, optional  device int32 [B], clamped into 0..kk: the first n_commit[b] tokens enter the cache
+ *                (NULL: all; 0: nothing changes).  All kk outputs are produced.
+ *   workspace    linattn_window_step_workspace_bytes(desc, kk) bytes (may be 0); used by one call at a time */
+size_t linattn_window_step_workspace_bytes(const linattn_window_desc *desc, int32_t kk);
+linattn_status linattn_window_step(const linattn_window_desc *desc, int32_t kk,
+                                   const void *q, const void *k, const void *v,
+                                   void *kcache, void *vcache, int32_t *pos, const int32_t *n_commit,
+                                   void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* What happens when the kernels' own synchronisation fails.  The waves of a bf16 prefill workgroup hand each
  * other data through LDS and wait for one another with bounded polling, so that a logic error or an extreme

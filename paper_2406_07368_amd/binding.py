@@ -28,6 +28,7 @@ PHI = {"elu1": LINATTN_PHI_ELU1, "relu": LINATTN_PHI_RELU}
 MAX_CONV_K, MAX_CONV_K_PREFILL, MAX_DRAFT, MAX_TREE = 8, 63, 16, 64
 SYMBOLS = ("linattn_workspace_bytes", "linattn_prefill", "linattn_prefill_noalloc", "linattn_noalloc_scratch_bytes", "linattn_prefill_grouped", "linattn_backward_workspace_bytes", "linattn_prefill_grouped_backward", "linattn_verify", "linattn_verify_grouped", "linattn_verify_tree", "linattn_decode",
            "linattn_decay_workspace_bytes", "linattn_decay_backward_workspace_bytes", "linattn_decay_prefill", "linattn_decay_backward", "linattn_decay_step",
+           "linattn_window_prefill", "linattn_window_backward_workspace_bytes", "linattn_window_backward", "linattn_window_step_workspace_bytes", "linattn_window_step",
            "linattn_set_wait_limit", "linattn_status_string", "linattn_version")
 
 
@@ -53,6 +54,12 @@ class Strides(ctypes.Structure):
 class DecayDesc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                *[(n, Strides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]]
+
+
+class WindowDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float),
                 *[(n, Strides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]]
 
 
@@ -95,6 +102,13 @@ def load():
     for f, args in ((lib.linattn_decay_prefill, [dd, i32] + [vp] * 8 + [vp, sz, vp]),
                     (lib.linattn_decay_backward, [dd, i32] + [vp] * 9 + [vp, sz, vp]),
                     (lib.linattn_decay_step, [dd, i32] + [vp] * 7 + [vp])):
+        f.restype, f.argtypes = ctypes.c_int, args
+    wd = ctypes.POINTER(WindowDesc)
+    for f in (lib.linattn_window_backward_workspace_bytes, lib.linattn_window_step_workspace_bytes):
+        f.restype, f.argtypes = sz, [wd, i32]
+    for f, args in ((lib.linattn_window_prefill, [wd, i32] + [vp] * 10),
+                    (lib.linattn_window_backward, [wd, i32] + [vp] * 10 + [vp, sz, vp]),
+                    (lib.linattn_window_step, [wd, i32] + [vp] * 8 + [vp, sz, vp])):
         f.restype, f.argtypes = ctypes.c_int, args
     lib.linattn_status_string.restype = ctypes.c_char_p
     lib.linattn_status_string.argtypes = [ctypes.c_int]
@@ -196,6 +210,12 @@ def make_decay_desc(B, H, d, io_dtype=torch.bfloat16, scale=1.0, **strides) -> D
     """strides: (b, h, t) in elements for each of q, k, v, out (prefill) and dout, dq, dk, dv (gradient) that the call takes."""
     code = {torch.float32: LINATTN_F32, torch.bfloat16: LINATTN_BF16}[io_dtype]
     return DecayDesc(B, H, d, code, float(scale), 0, **{n: Strides(*[int(x) for x in s]) for n, s in strides.items()})
+
+
+def make_window_desc(B, H, H_kv, d, window, sinks=0, io_dtype=torch.bfloat16, scale=1.0, **strides) -> WindowDesc:
+    """strides: as for ``make_decay_desc``."""
+    code = {torch.float32: LINATTN_F32, torch.bfloat16: LINATTN_BF16}[io_dtype]
+    return WindowDesc(B, H, H_kv, d, code, int(window), int(sinks), float(scale), **{n: Strides(*[int(x) for x in s]) for n, s in strides.items()})
 
 
 def linattn_set_wait_limit(spins: int) -> int:
@@ -300,6 +320,32 @@ def linattn_decay_step(desc: DecayDesc, kk, q, k, v, log_decay, S, n_commit, out
     st = load().linattn_decay_step(ctypes.byref(desc), int(kk), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(S), _ptr(n_commit), _ptr(out),
                                    _stream(stream))
     _check(st, "linattn_decay_step")
+
+
+def linattn_window_prefill(desc: WindowDesc, L, q, k, v, lens, out, lse=None, kcache=None, vcache=None, pos=None, stream=None) -> None:
+    st = load().linattn_window_prefill(ctypes.byref(desc), int(L), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(out), _ptr(lse), _ptr(kcache),
+                                       _ptr(vcache), _ptr(pos), _stream(stream))
+    _check(st, "linattn_window_prefill")
+
+
+def linattn_window_backward_workspace_bytes(desc: WindowDesc, L) -> int:
+    return int(load().linattn_window_backward_workspace_bytes(ctypes.byref(desc), int(L)))
+
+
+def linattn_window_backward(desc: WindowDesc, L, q, k, v, lens, out, lse, dout, dq, dk, dv, workspace, workspace_bytes=None, stream=None) -> None:
+    st = load().linattn_window_backward(ctypes.byref(desc), int(L), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq),
+                                        _ptr(dk), _ptr(dv), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+    _check(st, "linattn_window_backward")
+
+
+def linattn_window_step_workspace_bytes(desc: WindowDesc, kk) -> int:
+    return int(load().linattn_window_step_workspace_bytes(ctypes.byref(desc), int(kk)))
+
+
+def linattn_window_step(desc: WindowDesc, kk, q, k, v, kcache, vcache, pos, n_commit, out, workspace=None, workspace_bytes=None, stream=None) -> None:
+    st = load().linattn_window_step(ctypes.byref(desc), int(kk), _ptr(q), _ptr(k), _ptr(v), _ptr(kcache), _ptr(vcache), _ptr(pos), _ptr(n_commit),
+                                    _ptr(out), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+    _check(st, "linattn_window_step")
 
 
 # ---- conveniences that only allocate with torch and forward to the calls above ---------------
@@ -544,4 +590,81 @@ def decay_step(q, k, v, log_decay, state, scale=None, n_commit=None, stream=None
         out = torch.empty_like(q)
         desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale)
         linattn_decay_step(desc, kk, q, k, v, log_decay, state, n_commit, out, stream)
+    return out
+
+
+def _kv(where, q, k, v):
+    """Key/value rows [B,H_kv,L,d] for queries [B,H,L,d]."""
+    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.shape[1] < 1 or q.shape[1] % k.shape[1]:
+        raise ValueError(f"{where}: k and v must have one shape, q's with a number of heads that divides q's")
+
+
+def window_cache(B, H_kv, d, window, sinks=0, dtype=torch.bfloat16, device="cuda"):
+    """Cache of ``window_step`` for sequences that have not begun: (kcache, vcache, pos)."""
+    rows = [torch.empty((B, H_kv, sinks + window, d), dtype=dtype, device=device) for _ in range(2)]
+    return (*rows, torch.zeros((B, H_kv), dtype=torch.int32, device=device))
+
+
+def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=False, want_cache=False, stream=None):
+    """Softmax attention in which token t sees token s where s <= t and (s > t - window or s < sinks).
+
+    q: [B,H,L,d], k, v: [B,H_kv,L,d] (H_kv divides H: query head h uses key/value head h // (H // H_kv)), fp32 or bf16, of
+    any strides that are contiguous along d.  scale: None for d ** -0.5.  lens: None, or int32 [B], the tokens of each
+    row; rows behind them are ignored and their outputs are zeros.  sinks: at most 64.  Returns out, the logarithms of the
+    softmax sums (fp32 [B,H,L], what ``window_backward`` takes; None if not wanted) and the cache for ``window_step``
+    (kcache, vcache, pos; None if not wanted)."""
+    _rows("window_prefill", q, k=k, v=v)
+    _kv("window_prefill", q, k, v)
+    B, H, L, d = q.shape
+    _aux("window_prefill", "lens", lens, torch.int32, (B,), q.device)
+    with _on(q.device):
+        out = _like(q)
+        lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
+        cache = window_cache(B, k.shape[1], d, window, sinks, q.dtype, q.device) if want_cache else None
+        desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v), out=_st(out))
+        linattn_window_prefill(desc, L, q, k, v, lens, out, lse, *(cache or (None, None, None)), stream)
+    return out, lse, cache
+
+
+def window_backward(q, k, v, out, lse, dout, window, sinks=0, scale=None, lens=None, stream=None):
+    """Gradient of ``window_prefill`` with respect to q, k and v: bf16 rows, out and lse as it returned them, dout [B,H,L,d].
+    Returns dq, dk, dv (dk, dv summed over the query heads that share a key/value head)."""
+    _rows("window_backward", q, k=k, v=v, out=out, dout=dout)
+    _kv("window_backward", q, k, v)
+    B, H, L, d = q.shape
+    if out.shape != q.shape or dout.shape != q.shape:
+        raise ValueError("window_backward: out and dout must have q's shape")
+    if lse is None:
+        raise ValueError("window_backward: lse is what window_prefill returns with want_lse=True")
+    _aux("window_backward", "lse", lse, torch.float32, (B, H, L), q.device)
+    _aux("window_backward", "lens", lens, torch.int32, (B,), q.device)
+    with _on(q.device):
+        dq, dk, dv = _like(q), _like(k), _like(v)
+        desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v),
+                                out=_st(out), dout=_st(dout), dq=_st(dq), dk=_st(dk), dv=_st(dv))
+        ws = _scratch(linattn_window_backward_workspace_bytes(desc, L), q.device, stream)
+        linattn_window_backward(desc, L, q, k, v, lens, out, lse, dout, dq, dk, dv, ws, None, stream)
+    return dq, dk, dv
+
+
+def window_step(q, k, v, cache, window, sinks=0, scale=None, n_commit=None, stream=None):
+    """kk tokens (1..16) behind a cache: q dense [B,H,kk,d], k, v dense [B,H_kv,kk,d]; ``cache`` (kcache, vcache, pos) of
+    ``window_prefill`` or ``window_cache`` with the same window and sinks advances in place over the first n_commit[b]
+    (int32 [B]; None: all) of them.  Returns out."""
+    _rows("window_step", q, k=k, v=v)
+    _kv("window_step", q, k, v)
+    B, H, kk, d = q.shape
+    kcache, vcache, pos = cache
+    for n, x in (("q", q), ("k", k), ("v", v)):
+        if not x.is_contiguous():
+            raise ValueError(f"window_step: {n} must be dense")
+    for n, x in (("kcache", kcache), ("vcache", vcache)):
+        _aux("window_step", n, x, q.dtype, (B, k.shape[1], sinks + window, d), q.device)
+    _aux("window_step", "pos", pos, torch.int32, (B, k.shape[1]), q.device)
+    _aux("window_step", "n_commit", n_commit, torch.int32, (B,), q.device)
+    with _on(q.device):
+        out = torch.empty_like(q)
+        desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale)
+        ws = _scratch(linattn_window_step_workspace_bytes(desc, kk), q.device, stream)
+        linattn_window_step(desc, kk, q, k, v, kcache, vcache, pos, n_commit, out, ws, None, stream)
     return out

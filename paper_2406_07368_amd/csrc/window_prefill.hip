@@ -1,0 +1,198 @@
+// Softmax attention over a sliding window with sinks, bf16 rows, on the matrix cores.
+//
+//   out_t = sum_s p_ts v_s / sum_s p_ts,   p_ts = exp(scale q_t.k_s - m_t),   s <= t and (s > t - window or s < sinks)
+//
+// One pass over the visible keys with a running maximum m and a running sum.  A workgroup takes 128 queries of a head,
+// a wave 32 of them; 64 keys at a time lie in one of two LDS buffers while the next 64 are on their way in registers.
+// S^T = K Q^T with the keys in the accumulator's rows and a query per lane, so a query's statistics are a lane's own
+// (and its partner's 32 lanes on), and the weights, packed to bf16, are the operand of O^T += V^T P^T as they stand: the
+// accumulator layout is the operand layout up to a permutation of the keys, which is applied to the transposed reads of
+// V.  Key tiles that no query of the tile sees are not visited; masks are computed only where a border crosses.
+//
+// Bound: the matrix cores (4 d flops a visible pair) with the exponentials beside them.
+#include "common.h"
+#include "kernels.h"
+#include "mfma_util.h"
+#include "window.h"
+
+namespace linattn {
+
+namespace {
+
+constexpr int QT = 128, KT = 64;
+
+template <int D>
+struct Cfg {
+  static constexpr int RS = D + 16;
+  static constexpr int BUF = 2 * KT * RS;       // elements: K, V
+  static constexpr int BYTES = 2 * BUF * 2;
+  static constexpr int OS = D + 8;              // finished rows
+  static constexpr int PPR = D / 8;
+  static constexpr int NP = KT * PPR / 256;
+  static_assert(QT * OS <= 2 * BUF, "the finished rows take the buffers' place");
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a, int n) {
+  using G = Cfg<D>;
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
+  const int place = xcd_place(blockIdx.x, n);
+  if (place >= n) return;
+  const int tid = threadIdx.x;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  // the query heads that share keys side by side, then the query tiles
+  const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
+  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
+  const int b = bk / a.Hkv, hk = bk % a.Hkv, h = hk * group + g;
+  const int len = clamp_len(a.lens, b, a.L);
+  const int t0 = tile * QT, t_end = t0 + QT < a.L ? t0 + QT : a.L;
+  uint16_t* gout = const_cast<uint16_t*>(static_cast<const uint16_t*>(a.out.p)) + b * a.out.b + h * a.out.h;
+  float* glse = a.lse ? a.lse + ((int64_t)b * a.H + h) * a.L : nullptr;
+  if (t0 >= len) {                              // behind the end of the sequence
+    for (int e = tid; e < (t_end - t0) * G::PPR; e += 256) {
+      const u32x4 z = {0u, 0u, 0u, 0u};
+      *reinterpret_cast<u32x4*>(gout + (t0 + e / G::PPR) * a.out.t + e % G::PPR * 8) = z;
+    }
+    if (glse)
+      for (int t = t0 + tid; t < t_end; t += 256) glse[t] = -__builtin_inff();
+    return;
+  }
+  const uint16_t* gq = static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h;
+  const uint16_t* gk = static_cast<const uint16_t*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const uint16_t* gv = static_cast<const uint16_t*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const float c = window_log2_scale(a.scale);
+
+  const int t = t0 + 32 * w + l32;              // this lane's query
+  const int tw = t0 + 32 * w;                   // the wave's first
+  bf16x8 qop[D / 16];
+  {
+    const uint16_t* p = gq + (t < len ? t : len - 1) * a.q.t + 8 * hi;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qop[ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
+  }
+  // key tiles: those of the sinks that lie before the window's, then the window's
+  const int last = (t_end < len ? t_end : len) - 1;
+  const int lo = (t0 - a.window + 1 > 0 ? t0 - a.window + 1 : 0) / KT;
+  const int ns = a.sinks > 0 && lo > 0 ? 1 : 0; // (64 sinks at most: one tile)
+  const int nk = ns + last / KT - lo + 1;
+  auto key0 = [&](int i) { return (i < ns ? i : lo + i - ns) * KT; };
+
+  u32x4 rk[G::NP], rv[G::NP];
+  auto request = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < G::NP; ++i) {
+      const int p = tid + 256 * i, s = s0 + p / G::PPR, e = p % G::PPR * 8;
+      const int row = s < len ? s : 0;
+      rk[i] = *reinterpret_cast<const u32x4*>(gk + row * a.k.t + e);
+      rv[i] = *reinterpret_cast<const u32x4*>(gv + row * a.v.t + e);
+    }
+  };
+  auto put = [&](int s0, uint16_t* buf) {
+#pragma unroll
+    for (int i = 0; i < G::NP; ++i) {
+      const int p = tid + 256 * i;
+      uint16_t* d = buf + p / G::PPR * G::RS + p % G::PPR * 8;
+      const u32x4 z = {0u, 0u, 0u, 0u};
+      const bool in = s0 + p / G::PPR < len;
+      *reinterpret_cast<u32x4*>(d) = in ? rk[i] : z;
+      *reinterpret_cast<u32x4*>(d + KT * G::RS) = in ? rv[i] : z;
+    }
+  };
+
+  f32x16 O[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) O[i] = f32x16{};
+  float m = -__builtin_inff(), l = 0.f;         // l: this lane's half of the keys
+
+  request(key0(0));
+  put(key0(0), smem);
+  for (int i = 0; i < nk; ++i) {
+    const int s0 = key0(i);
+    const uint16_t *Kl = smem + (i & 1) * G::BUF, *Vl = Kl + KT * G::RS;
+    __syncthreads();
+    if (i + 1 < nk) request(key0(i + 1));
+    const bool some = s0 <= tw + 31 && (s0 + KT - 1 > tw - a.window || s0 < a.sinks);
+    if (some) {
+      f32x16 x[2] = {};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) x[kt] = mfma(lds_row8(Kl + (32 * kt + l32) * G::RS + 16 * ks + 8 * hi), qop[ks], x[kt]);
+      const bool all = s0 + KT - 1 <= tw && (s0 > tw + 31 - a.window || s0 + KT <= a.sinks);
+      if (!all) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!window_sees(t, s0 + 32 * kt + acc_row(r, hi), a.window, a.sinks)) x[kt][r] = -__builtin_inff();
+      }
+      float top = x[0][0];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, x[kt][r]);
+      const float m2 = fmaxf(m, max_xor32(top) * c);
+      const float mm = m2 == -__builtin_inff() ? 0.f : m2;     // nothing seen yet: every weight is exp2(-inf)
+      const float f = __builtin_amdgcn_exp2f(m - mm);
+      m = m2;
+      float sum = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          x[kt][r] = __builtin_amdgcn_exp2f(x[kt][r] * c - mm);
+          sum += x[kt][r];
+        }
+      l = l * f + sum;
+      if (__any(f != 1.f)) {
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) O[ct] *= f;
+      }
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8 p = pack8(x[kt], 8 * half);
+#pragma unroll
+          for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(tr_operand_acc_order(Vl, G::RS, 32 * kt + 16 * half, 32 * ct, lane), p, O[ct]);
+        }
+    }
+    if (i + 1 < nk) put(key0(i + 1), smem + ((i + 1) & 1) * G::BUF);
+  }
+
+  l = add_xor32(l);
+  const bool in = t < len;
+  const float inv = in ? 1.f / l : 0.f;
+  if (glse && hi == 0 && t < t_end) glse[t] = in ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -__builtin_inff();
+  __syncthreads();
+#pragma unroll
+  for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      u32x2 y = {pack_bf16x2(O[ct][4 * r4] * inv, O[ct][4 * r4 + 1] * inv), pack_bf16x2(O[ct][4 * r4 + 2] * inv, O[ct][4 * r4 + 3] * inv)};
+      *reinterpret_cast<u32x2*>(smem + (32 * w + l32) * G::OS + 32 * ct + 8 * r4 + 4 * hi) = y;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < QT * G::PPR / 256; ++i) {
+    const int p = tid + 256 * i, r = p / G::PPR;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(smem + r * G::OS + p % G::PPR * 8), z = {0u, 0u, 0u, 0u};
+    if (t0 + r < t_end) *reinterpret_cast<u32x4*>(gout + (t0 + r) * a.out.t + p % G::PPR * 8) = t0 + r < len ? x : z;
+  }
+}
+
+template <int D>
+hipError_t launch(const WindowArgs& a, hipStream_t s) {
+  const int n = a.B * a.H * ((a.L + QT - 1) / QT);
+  hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_kernel<D>), Cfg<D>::BYTES);
+  if (e != hipSuccess) return e;
+  window_prefill_kernel<D><<<dim3((n + 7) / 8 * 8), 256, Cfg<D>::BYTES, s>>>(a, n);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_window_prefill_bf16(const WindowArgs& a, int d, hipStream_t s) { return d == 64 ? launch<64>(a, s) : launch<128>(a, s); }
+
+}  // namespace linattn

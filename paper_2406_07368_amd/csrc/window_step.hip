@@ -1,0 +1,383 @@
+// Steps of softmax attention over a sliding window with sinks: kk tokens behind a cache of rows.
+//
+// The cache of a key/value head holds token s < sinks in row s and any other in row sinks + (s - sinks) % window, so at
+// most sinks + window rows however long the sequence.  With `pos` tokens seen, ring row r holds the token of age
+// (pos - sinks - 1 - r) mod window (0 = the newest), if that many went into the ring; token pos + j sees ages below
+// window - 1 - j, the sinks, and the step's own tokens up to itself.
+//
+// The cache is read once whatever the number of query heads that share it and of tokens: their R = (H / H_kv) kk rows are
+// the 32 columns of one product (32 at a time).  Tiles of 32 rows -- the step's own tokens are tile 0 -- go round over the
+// waves of the workgroups of a head, each with a running maximum and sum of its own and no barrier on the way: S^T = K Q^T
+// with the keys straight from memory as the operand, then O^T += V^T P^T with the weights as they stand (bf16 rows of V
+// through a wave's own LDS for the transposed reads; fp32 rows straight from memory, on the fp32 matrix instructions).
+// The waves' sums are joined in LDS, the workgroups' by a second launch, which also moves the kept tokens into the cache;
+// where a head has one workgroup, that does it itself.
+//
+// Bound: HBM (4 d bytes of cache row a token and key/value head in bf16).
+#include "common.h"
+#include "kernels.h"
+#include "mfma_util.h"
+#include "window.h"
+
+namespace linattn {
+
+namespace {
+
+constexpr int KT = 32;
+constexpr float kNone = -1e30f;                  // the maximum over nothing: finite, so that differences are numbers
+
+template <int D>
+struct MatBf16 {
+  typedef uint16_t elem;
+  typedef IoBf16 io;
+  static constexpr int RS = D + 16;
+  static constexpr int LDS = KT * RS * 2;        // bytes per wave
+  bf16x8 q[D / 16], k[D / 16];
+  u32x4 v[D / 16];
+  static constexpr int PPR = D / 8;
+  __device__ __forceinline__ void load_q(const elem* row, int hi) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const bf16x8*>(row + 16 * i + 8 * hi);
+  }
+  // key row `key` of this lane; value rows base .. base + 31, those from `rows` on are not there
+  __device__ __forceinline__ void request(const elem* kb, const elem* vb, int key, int base, int rows, int lane) {
+    const elem* kr = kb + (int64_t)key * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) k[i] = *reinterpret_cast<const bf16x8*>(kr + 16 * i);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const int p = lane + 64 * i, r = p / PPR;
+      v[i] = *reinterpret_cast<const u32x4*>(vb + (int64_t)(r < rows ? base + r : 0) * D + p % PPR * 8);
+    }
+  }
+  __device__ __forceinline__ f32x16 scores() const {
+    f32x16 x = {};
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x = mfma(k[i], q[i], x);
+    return x;
+  }
+  __device__ __forceinline__ void add(f32x16 (&O)[D / 32], const f32x16& p, unsigned char* lds, int rows, int lane) {
+    uint16_t* Vl = reinterpret_cast<uint16_t*>(lds);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const int e = lane + 64 * i;
+      *reinterpret_cast<u32x4*>(Vl + e / PPR * RS + e % PPR * 8) = e / PPR < rows ? v[i] : u32x4{0u, 0u, 0u, 0u};
+    }
+    __builtin_amdgcn_wave_barrier();             // (one wave: its LDS operations are served in order)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8 w = pack8(p, 8 * half);
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(tr_operand_acc_order(Vl, RS, 16 * half, 32 * ct, lane), w, O[ct]);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
+template <int D>
+struct MatF32 {
+  typedef float elem;
+  typedef IoF32 io;
+  static constexpr int LDS = 0;
+  f32x4 q[D / 8], k[D / 8];
+  float v[16][D / 32];
+  __device__ __forceinline__ void load_q(const elem* row, int hi) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) q[i] = *reinterpret_cast<const f32x4*>(row + D / 2 * hi + 4 * i);
+  }
+  __device__ __forceinline__ void request(const elem* kb, const elem* vb, int key, int base, int rows, int lane) {
+    const elem* kr = kb + (int64_t)key * D + D / 2 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) k[i] = *reinterpret_cast<const f32x4*>(kr + 4 * i);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = acc_row(r, lane >> 5);
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct) v[r][ct] = vb[(int64_t)(row < rows ? base + row : 0) * D + 32 * ct + (lane & 31)];
+    }
+  }
+  __device__ __forceinline__ f32x16 scores() const {
+    f32x16 x = {};
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i][e], q[i][e], x, 0, 0, 0);
+    return x;
+  }
+  __device__ __forceinline__ void add(f32x16 (&O)[D / 32], const f32x16& p, unsigned char*, int rows, int lane) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const bool in = acc_row(r, lane >> 5) < rows;
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct) O[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? v[r][ct] : 0.f, p[r], O[ct], 0, 0, 0);
+    }
+  }
+};
+
+__device__ __forceinline__ int kept(const int32_t* n_commit, int b, int kk) {
+  if (!n_commit) return kk;
+  const int n = n_commit[b];
+  return n < 0 ? 0 : n > kk ? kk : n;
+}
+
+// the first n of the step's tokens -> the cache (a token that a later one of them replaces is left out)
+template <typename E, int D>
+__device__ void commit(const WindowStepArgs& a, int bk, int pos, int n, int tid) {
+  constexpr int PPR = D * sizeof(E) / 16, EP = 16 / sizeof(E);
+  const int64_t held = (int64_t)a.sinks + a.window;
+  for (int e = tid; e < 2 * n * PPR; e += 256) {
+    const int kv = e / (n * PPR), j = e / PPR % n, c = e % PPR * EP;
+    const int64_t at = (int64_t)pos + j;
+    if (at >= a.sinks && at + a.window < (int64_t)pos + n) continue;
+    const int64_t row = at < a.sinks ? at : a.sinks + (at - a.sinks) % a.window;
+    const E* from = static_cast<const E*>(kv ? a.v : a.k) + ((int64_t)bk * a.kk + j) * D + c;
+    E* to = static_cast<E*>(kv ? a.vcache : a.kcache) + (bk * held + row) * D + c;
+    *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(from);
+  }
+  if (tid == 0) a.pos[bk] = pos + n;
+}
+
+template <template <int> class M, int D>
+__global__ __launch_bounds__(256) void window_step_kernel(WindowStepArgs a) {
+  typedef typename M<D>::elem E;
+  constexpr int JOIN = 2 * (D / 2 + 2) * 64 * 4;     // two waves' accumulators, maxima, sums
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
+  static_assert(JOIN > 0, "");
+  const int tid = threadIdx.x;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int split = blockIdx.x % a.nsplit, bk = blockIdx.x / a.nsplit;
+  const int b = bk / a.Hkv, hk = bk % a.Hkv, group = a.H / a.Hkv, R = group * a.kk;
+  const int r0 = 32 * blockIdx.y, row = r0 + l32;    // this lane's query row: head row / kk of the group, token row % kk
+  const int j = row % a.kk;
+  int pos = a.pos[bk];
+  pos = pos < 0 ? 0 : pos;
+  const int64_t held = (int64_t)a.sinks + a.window;
+  const int live = pos < held ? pos : (int)held;     // cache rows in use
+  const int nt = (live + KT - 1) / KT + 1;
+  const E* kc = static_cast<const E*>(a.kcache) + bk * held * D;
+  const E* vc = static_cast<const E*>(a.vcache) + bk * held * D;
+  const E* kn = static_cast<const E*>(a.k) + (int64_t)bk * a.kk * D;
+  const E* vn = static_cast<const E*>(a.v) + (int64_t)bk * a.kk * D;
+  const int64_t qrow = ((int64_t)b * a.H + hk * group) * a.kk;
+  const float c = window_log2_scale(a.scale);
+  unsigned char* lds = smem_b + w * M<D>::LDS;
+
+  M<D> mat;
+  mat.load_q(static_cast<const E*>(a.q) + (qrow + (row < R ? row : R - 1)) * D, hi);
+  f32x16 O[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) O[i] = f32x16{};
+  float m = kNone, l = 0.f;
+  const int ring = pos - a.sinks;                    // tokens that went into the ring (or less than 0)
+  for (int i = split * 4 + w; i < nt; i += a.nsplit * 4) {
+    const int s0 = (i - 1) * KT;                     // the tile's first cache row
+    const int rows = i == 0 ? a.kk : live - s0 < KT ? live - s0 : KT;
+    if (i == 0) mat.request(kn, vn, l32 < a.kk ? l32 : 0, 0, rows, lane);
+    else mat.request(kc, vc, l32 < rows ? s0 + l32 : 0, s0, rows, lane);
+    f32x16 x = mat.scores();
+    if (i == 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int s = acc_row(r, hi);
+        if (!(s <= j && (s > j - a.window || pos + s < a.sinks))) x[r] = -__builtin_inff();
+      }
+    } else {
+      // age of the tile's first row if it is a ring row; the next rows' are smaller by one each, round the ring
+      int age0 = (ring - 1 - (s0 - a.sinks)) % a.window;
+      if (age0 < 0) age0 += a.window;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int u = acc_row(r, hi);
+        int age = age0 - u;
+        if (age < 0) age += a.window;
+        if (a.window < KT && age < 0) age = (age0 - u) % a.window + ((age0 - u) % a.window < 0 ? a.window : 0);
+        const bool sees = s0 + u < a.sinks ? s0 + u < pos : age < ring && age < a.window - 1 - j;
+        if (!sees || u >= rows) x[r] = -__builtin_inff();
+      }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
+    const float m2 = fmaxf(m, max_xor32(top) * c);
+    const float f = __builtin_amdgcn_exp2f(m - m2);
+    m = m2;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(x[r] * c - m2);
+      sum += x[r];
+    }
+    l = l * f + sum;
+    if (__any(f != 1.f)) {
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct) O[ct] *= f;
+    }
+    mat.add(O, x, lds, rows, lane);
+  }
+  l = add_xor32(l);
+
+  // the waves' sums: 2, 3 into 0, 1, then 1 into 0
+  float* jl = reinterpret_cast<float*>(smem_b);
+#pragma unroll
+  for (int half = 2; half >= 1; half /= 2) {
+    __syncthreads();
+    if (w >= half && w < 2 * half) {
+      float* p = jl + (w - half) * (D / 2 + 2) * 64 + lane;
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[(16 * ct + r) * 64] = O[ct][r];
+      p[D / 2 * 64] = m;
+      p[(D / 2 + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (w < half) {
+      const float* p = jl + w * (D / 2 + 2) * 64 + lane;
+      const float mo = p[D / 2 * 64], m2 = fmaxf(m, mo);
+      const float f = __builtin_amdgcn_exp2f(m - m2), fo = __builtin_amdgcn_exp2f(mo - m2);
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[ct][r] = O[ct][r] * f + p[(16 * ct + r) * 64] * fo;
+      l = l * f + p[(D / 2 + 1) * 64] * fo;
+      m = m2;
+    }
+  }
+  if (w == 0 && row < R) {
+    if (a.nsplit == 1) {
+      const float inv = 1.f / l;
+      E* o = static_cast<E*>(a.out) + (qrow + row) * D;
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int e = 32 * ct + 8 * r4 + 4 * hi;
+          const float y[4] = {O[ct][4 * r4] * inv, O[ct][4 * r4 + 1] * inv, O[ct][4 * r4 + 2] * inv, O[ct][4 * r4 + 3] * inv};
+          if constexpr (sizeof(E) == 2) *reinterpret_cast<u32x2*>(o + e) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+          else *reinterpret_cast<f32x4*>(o + e) = f32x4{y[0], y[1], y[2], y[3]};
+        }
+    } else {
+      const int64_t at = ((int64_t)bk * a.nsplit + split) * R + row;
+      float* stat = a.ws + (int64_t)a.B * a.Hkv * a.nsplit * R * D + 2 * at;
+      if (hi == 0) { stat[0] = m; stat[1] = l; }
+      float* o = a.ws + at * D;
+      if (l > 0.f) {
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4)
+            *reinterpret_cast<f32x4*>(o + 32 * ct + 8 * r4 + 4 * hi) = f32x4{O[ct][4 * r4], O[ct][4 * r4 + 1], O[ct][4 * r4 + 2], O[ct][4 * r4 + 3]};
+      }
+    }
+  }
+  // (every wave is behind the barriers above, so every read of the cache and of pos is done)
+  if (a.nsplit == 1 && gridDim.y == 1) commit<E, D>(a, bk, pos, kept(a.n_commit, b, a.kk), tid);
+}
+
+// the workgroups' sums; workgroup 0 of a head then moves the kept tokens into the cache
+template <typename IO, int D>
+__global__ __launch_bounds__(256) void window_join_kernel(WindowStepArgs a) {
+  typedef typename IO::elem E;
+  const int bk = blockIdx.x, b = bk / a.Hkv, hk = bk % a.Hkv, group = a.H / a.Hkv, R = group * a.kk;
+  const int64_t qrow = ((int64_t)b * a.H + hk * group) * a.kk;
+  const int e = blockIdx.y * 256 + threadIdx.x;      // four elements of a row
+  if (a.nsplit > 1 && e < R * (D / 4)) {
+    const int row = e / (D / 4), c = e % (D / 4) * 4;
+    const int64_t at = (int64_t)bk * a.nsplit * R + row;
+    const float* stat = a.ws + (int64_t)a.B * a.Hkv * a.nsplit * R * D + 2 * at;
+    float m = kNone;
+    for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, stat[2 * (int64_t)s * R]);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int s = 0; s < a.nsplit; ++s) {
+      const float lo = stat[2 * (int64_t)s * R + 1];
+      if (lo > 0.f) {
+        const float f = __builtin_amdgcn_exp2f(stat[2 * (int64_t)s * R] - m);
+        l += lo * f;
+        x += f * *reinterpret_cast<const f32x4*>(a.ws + (at + (int64_t)s * R) * D + c);
+      }
+    }
+    x *= 1.f / l;
+    E* o = static_cast<E*>(a.out) + (qrow + row) * D + c;
+    if constexpr (sizeof(E) == 2) *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    else *reinterpret_cast<f32x4*>(o) = x;
+  }
+  if (blockIdx.y == 0) {
+    int pos = a.pos[bk];
+    __syncthreads();
+    commit<E, D>(a, bk, pos < 0 ? 0 : pos, kept(a.n_commit, b, a.kk), threadIdx.x);
+  }
+}
+
+template <template <int> class M, int D>
+hipError_t launch(const WindowStepArgs& a, hipStream_t s) {
+  typedef typename M<D>::io IO;
+  constexpr int JOIN = 2 * (D / 2 + 2) * 64 * 4, LDS = 4 * M<D>::LDS > JOIN ? 4 * M<D>::LDS : JOIN;
+  const int R = a.H / a.Hkv * a.kk, blocks = (R + 31) / 32;
+  hipError_t e = LINATTN_MAX_LDS_ONCE((window_step_kernel<M, D>), LDS);
+  if (e != hipSuccess) return e;
+  window_step_kernel<M, D><<<dim3(a.B * a.Hkv * a.nsplit, blocks), 256, LDS, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || (a.nsplit == 1 && blocks == 1)) return e;
+  window_join_kernel<IO, D><<<dim3(a.B * a.Hkv, a.nsplit > 1 ? (R * (D / 4) + 255) / 256 : 1), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// ---- a prompt's last rows into the cache ---------------------------------------------------------------------------
+template <typename E, int D>
+__global__ __launch_bounds__(256) void window_cache_kernel(WindowCacheArgs a) {
+  constexpr int PPR = D * sizeof(E) / 16, EP = 16 / sizeof(E), PER = 256 / PPR;
+  const int bk = blockIdx.x, b = bk / a.Hkv, hk = bk % a.Hkv;
+  const int pos = clamp_len(a.lens, b, a.L);
+  const int64_t held = (int64_t)a.sinks + a.window;
+  const E* k = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const E* v = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const int c = threadIdx.x % PPR * EP;
+  const int64_t live = pos < held ? pos : held;
+  for (int64_t row = (int64_t)blockIdx.y * PER + threadIdx.x / PPR; row < live; row += (int64_t)gridDim.y * PER) {
+    int64_t s = row;                                 // the token whose place this row is
+    if (row >= a.sinks) {
+      const int64_t r = row - a.sinks, ring = (int64_t)pos - a.sinks;
+      s = a.sinks + ring - 1 - (ring - 1 - r) % a.window;   // (row < live: ring - 1 >= r or the ring is full)
+    }
+    const int64_t to = (bk * held + row) * D + c;
+    *reinterpret_cast<u32x4*>(static_cast<E*>(a.kcache) + to) = *reinterpret_cast<const u32x4*>(k + s * a.k.t + c);
+    *reinterpret_cast<u32x4*>(static_cast<E*>(a.vcache) + to) = *reinterpret_cast<const u32x4*>(v + s * a.v.t + c);
+  }
+  if (blockIdx.y == 0 && threadIdx.x == 0) a.pos[bk] = pos;
+}
+
+template <typename E, int D>
+hipError_t launch_cache(const WindowCacheArgs& a, hipStream_t s) {
+  constexpr int PER = 256 / (D * sizeof(E) / 16);
+  int64_t held = (int64_t)a.sinks + a.window;
+  if (held > a.L) held = a.L;
+  int64_t y = (held + 4 * PER - 1) / (4 * PER);      // four rows a thread
+  y = y < 1 ? 1 : y > 1024 ? 1024 : y;
+  window_cache_kernel<E, D><<<dim3(a.B * a.Hkv, (unsigned)y), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Workgroups per key/value head: enough that every compute unit has some (two of their waves' tile chains hide each
+// other's trips to memory), as long as every wave has a tile.
+int window_step_splits(int64_t heads, int64_t held, int rows) {
+  const int64_t wgs = heads * ((rows + 31) / 32), tiles = (held + KT - 1) / KT + 1;
+  int64_t n = (1024 + wgs - 1) / wgs;
+  if (n > (tiles + 3) / 4) n = (tiles + 3) / 4;
+  return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+}
+
+hipError_t launch_window_step(const WindowStepArgs& a, int d, bool bf16, hipStream_t s) {
+  if (bf16) return d == 64 ? launch<MatBf16, 64>(a, s) : launch<MatBf16, 128>(a, s);
+  return d == 64 ? launch<MatF32, 64>(a, s) : launch<MatF32, 128>(a, s);
+}
+
+hipError_t launch_window_cache(const WindowCacheArgs& a, int d, bool bf16, hipStream_t s) {
+  if (bf16) return d == 64 ? launch_cache<uint16_t, 64>(a, s) : launch_cache<uint16_t, 128>(a, s);
+  return d == 64 ? launch_cache<float, 64>(a, s) : launch_cache<float, 128>(a, s);
+}
+
+}  // namespace linattn
