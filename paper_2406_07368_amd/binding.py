@@ -146,8 +146,11 @@ def _native():
         if _calls is None:
             _calls = _load_calls()
         f = [lib.linattn_workspace_bytes, lib.linattn_prefill, lib.linattn_prefill_grouped, lib.linattn_backward_workspace_bytes,
-             lib.linattn_prefill_grouped_backward, lib.linattn_verify, lib.linattn_verify_grouped, lib.linattn_verify_tree, lib.linattn_decode]
-        _calls.bind(*[ctypes.cast(x, ctypes.c_void_p).value for x in f], torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+             lib.linattn_prefill_grouped_backward, lib.linattn_verify, lib.linattn_verify_grouped, lib.linattn_verify_tree, lib.linattn_decode,
+             lib.linattn_decay_workspace_bytes, lib.linattn_decay_prefill, lib.linattn_decay_backward_workspace_bytes, lib.linattn_decay_backward,
+             lib.linattn_decay_step, lib.linattn_window_prefill, lib.linattn_window_backward_workspace_bytes, lib.linattn_window_backward,
+             lib.linattn_window_step_workspace_bytes, lib.linattn_window_step]
+        _calls.bind(tuple(ctypes.cast(x, ctypes.c_void_p).value for x in f), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
         _bound = lib
     return _calls
 
@@ -542,6 +545,10 @@ def decay_prefill(q, k, v, log_decay, scale=None, state=None, lens=None, want_st
     state: None or the fp32 [B,H,d,d] to go on from.  lens: None, or int32 [B], the tokens of each row; rows behind
     them are ignored and their outputs are zeros.  Returns out (q's layout where q is dense in some order of its axes)
     and the new state (None if not wanted)."""
+    if stream is None:
+        r = _native().decay_prefill(q, k, v, log_decay, scale, state, lens, want_state)
+        if r is not None:
+            return _result(r, "linattn_decay_prefill")
     _rows("decay_prefill", q, k=k, v=v)
     B, H, L, d = q.shape
     if k.shape != q.shape or v.shape != q.shape:
@@ -561,6 +568,10 @@ def decay_prefill(q, k, v, log_decay, scale=None, state=None, lens=None, want_st
 def decay_backward(q, k, v, log_decay, dout, scale=None, lens=None, stream=None):
     """Gradient of ``decay_prefill`` (from no state) with respect to q, k and v; dout: [B,H,L,d], any strides that are
     contiguous along d.  Returns dq, dk, dv."""
+    if stream is None:
+        r = _native().decay_backward(q, k, v, log_decay, dout, scale, lens)
+        if r is not None:
+            return _result(r, "linattn_decay_backward")
     _rows("decay_backward", q, k=k, v=v, dout=dout)
     B, H, L, d = q.shape
     if k.shape != q.shape or v.shape != q.shape or dout.shape != q.shape:
@@ -579,6 +590,10 @@ def decay_backward(q, k, v, log_decay, dout, scale=None, lens=None, stream=None)
 def decay_step(q, k, v, log_decay, state, scale=None, n_commit=None, stream=None):
     """kk tokens (1..16) from a running state: q, k, v dense [B,H,kk,d]; ``state`` (fp32 [B,H,d,d]) advances in place over
     the first n_commit[b] (int32 [B]; None: all) of them.  Returns out."""
+    if stream is None:
+        r = _native().decay_step(q, k, v, log_decay, state, scale, n_commit)
+        if r is not None:
+            return _result(r, "linattn_decay_step")
     _rows("decay_step", q, k=k, v=v)
     B, H, kk, d = q.shape
     if k.shape != q.shape or v.shape != q.shape or not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
@@ -613,6 +628,10 @@ def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=Fal
     row; rows behind them are ignored and their outputs are zeros.  sinks: at most 64.  Returns out, the logarithms of the
     softmax sums (fp32 [B,H,L], what ``window_backward`` takes; None if not wanted) and the cache for ``window_step``
     (kcache, vcache, pos; None if not wanted)."""
+    if stream is None and not want_cache:
+        r = _native().window_prefill(q, k, v, window, sinks, scale, lens, want_lse)
+        if r is not None:
+            return _result(r, "linattn_window_prefill")
     _rows("window_prefill", q, k=k, v=v)
     _kv("window_prefill", q, k, v)
     B, H, L, d = q.shape
@@ -629,6 +648,10 @@ def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=Fal
 def window_backward(q, k, v, out, lse, dout, window, sinks=0, scale=None, lens=None, stream=None):
     """Gradient of ``window_prefill`` with respect to q, k and v: bf16 rows, out and lse as it returned them, dout [B,H,L,d].
     Returns dq, dk, dv (dk, dv summed over the query heads that share a key/value head)."""
+    if stream is None:
+        r = _native().window_backward(q, k, v, out, lse, dout, window, sinks, scale, lens)
+        if r is not None:
+            return _result(r, "linattn_window_backward")
     _rows("window_backward", q, k=k, v=v, out=out, dout=dout)
     _kv("window_backward", q, k, v)
     B, H, L, d = q.shape
@@ -651,6 +674,10 @@ def window_step(q, k, v, cache, window, sinks=0, scale=None, n_commit=None, stre
     """kk tokens (1..16) behind a cache: q dense [B,H,kk,d], k, v dense [B,H_kv,kk,d]; ``cache`` (kcache, vcache, pos) of
     ``window_prefill`` or ``window_cache`` with the same window and sinks advances in place over the first n_commit[b]
     (int32 [B]; None: all) of them.  Returns out."""
+    if stream is None:
+        r = _native().window_step(q, k, v, cache, window, sinks, scale, n_commit)
+        if r is not None:
+            return _result(r, "linattn_window_step")
     _rows("window_step", q, k=k, v=v)
     _kv("window_step", q, k, v)
     B, H, kk, d = q.shape

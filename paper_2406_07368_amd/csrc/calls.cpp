@@ -15,6 +15,8 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 
+#include <cmath>
+
 #include "../../include/linattn.h"
 
 namespace {
@@ -29,7 +31,18 @@ struct Library {
   decltype(&linattn_verify_grouped) verify_grouped = nullptr;
   decltype(&linattn_verify_tree) verify_tree = nullptr;
   decltype(&linattn_decode) decode = nullptr;
+  decltype(&linattn_decay_workspace_bytes) decay_workspace_bytes = nullptr;
+  decltype(&linattn_decay_prefill) decay_prefill = nullptr;
+  decltype(&linattn_decay_backward_workspace_bytes) decay_backward_workspace_bytes = nullptr;
+  decltype(&linattn_decay_backward) decay_backward = nullptr;
+  decltype(&linattn_decay_step) decay_step = nullptr;
+  decltype(&linattn_window_prefill) window_prefill = nullptr;
+  decltype(&linattn_window_backward_workspace_bytes) window_backward_workspace_bytes = nullptr;
+  decltype(&linattn_window_backward) window_backward = nullptr;
+  decltype(&linattn_window_step_workspace_bytes) window_step_workspace_bytes = nullptr;
+  decltype(&linattn_window_step) window_step = nullptr;
 } lib;
+constexpr int kFunctions = 19;
 PyObject *get_device = nullptr, *get_raw_stream = nullptr;   // torch._C._cuda_getDevice, _cuda_getCurrentRawStream
 
 // a call's arguments that the native path takes; any `false` below means: the general path
@@ -261,15 +274,232 @@ PyObject* py_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of the nine functions in the order of Library's members, _cuda_getDevice, _cuda_getCurrentRawStream)
+// ---- the operators with strides per tensor: what binding.py refuses takes its path, on which it is refused -------------
+// Rows [B,heads,L,d] of q's type on q's device, contiguous along d; q on the current device (binding.py switches devices).
+bool rows(const at::Tensor& x, const at::Tensor& q) {
+  return x.dim() == 4 && x.scalar_type() == q.scalar_type() && x.device() == q.device() && x.size(3) == q.size(3) && x.stride(3) == 1;
+}
+bool shaped(const at::Tensor* x, at::ScalarType type, at::IntArrayRef shape, const at::Tensor& q) {
+  return !x || (x->scalar_type() == type && x->sizes() == shape && x->device() == q.device() && x->is_contiguous());
+}
+bool small(PyObject* o, int32_t& x) {
+  if (!PyLong_CheckExact(o)) return false;
+  int over = 0;
+  const long y = PyLong_AsLongAndOverflow(o, &over);
+  if (over || y < INT32_MIN || y > INT32_MAX) return false;
+  x = (int32_t)y;
+  return true;
+}
+bool scale_of(PyObject* o, const at::Tensor& q, float& x) {
+  if (o == Py_None) { x = (float)std::pow((double)q.size(3), -0.5); return true; }
+  double y;
+  if (!number(o, y)) return false;
+  x = (float)y;
+  return true;
+}
+linattn_strides strides(const at::Tensor& x) {
+  auto s = [&](int i) { return x.size(i) < 2 ? 0 : x.stride(i); };
+  return {s(0), s(1), s(2)};
+}
+// the current stream, if the current device is q's; `other` where it is not
+bool stream_of(const at::Tensor& q, void*& s, bool& other) {
+  PyObject* dev = PyObject_CallNoArgs(get_device);
+  if (!dev) return false;
+  other = PyLong_AsLong(dev) != q.device().index();
+  PyObject* raw = other ? nullptr : PyObject_CallOneArg(get_raw_stream, dev);
+  Py_DECREF(dev);
+  if (other) return !PyErr_Occurred();
+  if (!raw) return false;
+  s = PyLong_AsVoidPtr(raw);
+  Py_DECREF(raw);
+  return !PyErr_Occurred();
+}
+at::Tensor scratch(size_t bytes, const at::Tensor& q) {
+  return bytes ? at::empty({(int64_t)bytes}, at::TensorOptions().device(q.device()).dtype(at::kByte)) : at::Tensor();
+}
+const at::Tensor* some(const at::Tensor& t) { return t.defined() ? &t : nullptr; }
+
+bool decay_desc(const at::Tensor& q, PyObject* scale, linattn_decay_desc& x) {
+  x = linattn_decay_desc{};
+  if (q.dim() != 4 || !io_type(q, x.io_dtype) || q.size(0) > INT32_MAX || q.size(1) > INT32_MAX || q.size(2) > INT32_MAX || !scale_of(scale, q, x.scale)) return false;
+  x.B = (int32_t)q.size(0); x.H = (int32_t)q.size(1); x.d = (int32_t)q.size(3);
+  return true;
+}
+
+// decay_prefill(q, k, v, log_decay, scale, state, lens, want_state) -> (out, state)
+PyObject* py_decay_prefill(PyObject*, PyObject* const* a, Py_ssize_t) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *g, *S, *lens;
+  linattn_decay_desc x;
+  if (!tensor(a[0], q) || !tensor(a[1], k) || !tensor(a[2], v) || !tensor(a[3], g) || !tensor_or_none(a[5], S) || !tensor_or_none(a[6], lens) || !PyBool_Check(a[7]) ||
+      !decay_desc(*q, a[4], x) || !rows(*q, *q) || !rows(*k, *q) || !rows(*v, *q) || k->sizes() != q->sizes() || v->sizes() != q->sizes())
+    Py_RETURN_NONE;
+  const int64_t B = x.B, H = x.H, L = q->size(2), d = x.d;
+  if (!shaped(g, at::kFloat, {H}, *q) || !shaped(S, at::kFloat, {B, H, d, d}, *q) || !shaped(lens, at::kInt, {B}, *q)) Py_RETURN_NONE;
+  void* s = nullptr;
+  bool other;
+  if (!stream_of(*q, s, other)) return nullptr;
+  if (other) Py_RETURN_NONE;
+  const at::Tensor out = at::empty_like(*q);
+  at::Tensor T;
+  if (a[7] == Py_True) T = at::empty({B, H, d, d}, at::TensorOptions().device(q->device()).dtype(at::kFloat));
+  x.q = strides(*q); x.k = strides(*k); x.v = strides(*v); x.out = strides(out);
+  const size_t bytes = lib.decay_workspace_bytes(&x, (int32_t)L);
+  const at::Tensor ws = scratch(bytes, *q);
+  const int st = without_gil(lib.decay_prefill, &x, (int32_t)L, ptr(q), ptr(k), ptr(v), ptr_as<float>(g), ptr_as<int32_t>(lens), ptr_as<float>(S), ptr(&out), ptr_as<float>(some(T)), ptr(some(ws)), bytes, s);
+  if (st != 0) return PyLong_FromLong(st);
+  return T.defined() ? Py_BuildValue("(NN)", THPVariable_Wrap(out), THPVariable_Wrap(T)) : Py_BuildValue("(NO)", THPVariable_Wrap(out), Py_None);
+  END_HANDLE_TH_ERRORS
+}
+
+// decay_backward(q, k, v, log_decay, dout, scale, lens) -> (dq, dk, dv)
+PyObject* py_decay_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *g, *dout, *lens;
+  linattn_decay_desc x;
+  if (!tensor(a[0], q) || !tensor(a[1], k) || !tensor(a[2], v) || !tensor(a[3], g) || !tensor(a[4], dout) || !tensor_or_none(a[6], lens) || !decay_desc(*q, a[5], x) ||
+      !rows(*q, *q) || !rows(*k, *q) || !rows(*v, *q) || !rows(*dout, *q) || k->sizes() != q->sizes() || v->sizes() != q->sizes() || dout->sizes() != q->sizes() ||
+      !shaped(g, at::kFloat, {q->size(1)}, *q) || !shaped(lens, at::kInt, {q->size(0)}, *q))
+    Py_RETURN_NONE;
+  void* s = nullptr;
+  bool other;
+  if (!stream_of(*q, s, other)) return nullptr;
+  if (other) Py_RETURN_NONE;
+  const int32_t L = (int32_t)q->size(2);
+  const at::Tensor dq = at::empty_like(*q), dk = at::empty_like(*k), dv = at::empty_like(*v);
+  x.q = strides(*q); x.k = strides(*k); x.v = strides(*v); x.dout = strides(*dout);
+  x.dq = strides(dq); x.dk = strides(dk); x.dv = strides(dv);
+  const size_t bytes = lib.decay_backward_workspace_bytes(&x, L);
+  const at::Tensor ws = scratch(bytes, *q);
+  const int st = without_gil(lib.decay_backward, &x, L, ptr(q), ptr(k), ptr(v), ptr_as<float>(g), ptr_as<int32_t>(lens), ptr(dout), ptr(&dq), ptr(&dk), ptr(&dv), ptr(some(ws)), bytes, s);
+  if (st != 0) return PyLong_FromLong(st);
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(dq), THPVariable_Wrap(dk), THPVariable_Wrap(dv));
+  END_HANDLE_TH_ERRORS
+}
+
+// decay_step(q, k, v, log_decay, state, scale, n_commit) -> out
+PyObject* py_decay_step(PyObject*, PyObject* const* a, Py_ssize_t) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *g, *S, *n;
+  linattn_decay_desc x;
+  if (!tensor(a[0], q) || !tensor(a[1], k) || !tensor(a[2], v) || !tensor(a[3], g) || !tensor(a[4], S) || !tensor_or_none(a[6], n) || !decay_desc(*q, a[5], x))
+    Py_RETURN_NONE;
+  const int64_t B = x.B, H = x.H, d = x.d;
+  for (const at::Tensor* t : {q, k, v})
+    if (!shaped(t, q->scalar_type(), q->sizes(), *q)) Py_RETURN_NONE;
+  if (!shaped(g, at::kFloat, {H}, *q) || !shaped(S, at::kFloat, {B, H, d, d}, *q) || !shaped(n, at::kInt, {B}, *q)) Py_RETURN_NONE;
+  void* s = nullptr;
+  bool other;
+  if (!stream_of(*q, s, other)) return nullptr;
+  if (other) Py_RETURN_NONE;
+  const at::Tensor out = at::empty_like(*q);
+  const int st = without_gil(lib.decay_step, &x, (int32_t)q->size(2), ptr(q), ptr(k), ptr(v), ptr_as<float>(g), ptr_as<float>(S), ptr_as<int32_t>(n), ptr(&out), s);
+  return out_or_status(st, out);
+  END_HANDLE_TH_ERRORS
+}
+
+bool window_desc(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, PyObject* window, PyObject* sinks, PyObject* scale, linattn_window_desc& x) {
+  x = linattn_window_desc{};
+  if (q.dim() != 4 || !io_type(q, x.io_dtype) || !rows(q, q) || !rows(k, q) || !rows(v, q) || k.sizes() != v.sizes() || k.size(0) != q.size(0) || k.size(2) != q.size(2) ||
+      k.size(1) < 1 || q.size(1) % k.size(1) || q.size(0) > INT32_MAX || q.size(1) > INT32_MAX || q.size(2) > INT32_MAX || !small(window, x.window) ||
+      !small(sinks, x.sinks) || !scale_of(scale, q, x.scale))
+    return false;
+  x.B = (int32_t)q.size(0); x.H = (int32_t)q.size(1); x.H_kv = (int32_t)k.size(1); x.d = (int32_t)q.size(3);
+  x.q = strides(q); x.k = strides(k); x.v = strides(v);
+  return true;
+}
+
+// window_prefill(q, k, v, window, sinks, scale, lens, want_lse) -> (out, lse, None)
+PyObject* py_window_prefill(PyObject*, PyObject* const* a, Py_ssize_t) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *lens;
+  linattn_window_desc x;
+  if (!tensor(a[0], q) || !tensor(a[1], k) || !tensor(a[2], v) || !tensor_or_none(a[6], lens) || !PyBool_Check(a[7]) || !window_desc(*q, *k, *v, a[3], a[4], a[5], x) ||
+      !shaped(lens, at::kInt, {q->size(0)}, *q))
+    Py_RETURN_NONE;
+  void* s = nullptr;
+  bool other;
+  if (!stream_of(*q, s, other)) return nullptr;
+  if (other) Py_RETURN_NONE;
+  const at::Tensor out = at::empty_like(*q);
+  at::Tensor lse;
+  if (a[7] == Py_True) lse = at::empty({q->size(0), q->size(1), q->size(2)}, at::TensorOptions().device(q->device()).dtype(at::kFloat));
+  x.out = strides(out);
+  const int st = without_gil(lib.window_prefill, &x, (int32_t)q->size(2), ptr(q), ptr(k), ptr(v), ptr_as<int32_t>(lens), ptr(&out), ptr_as<float>(some(lse)), nullptr, nullptr, nullptr, s);
+  if (st != 0) return PyLong_FromLong(st);
+  return lse.defined() ? Py_BuildValue("(NNO)", THPVariable_Wrap(out), THPVariable_Wrap(lse), Py_None) : Py_BuildValue("(NOO)", THPVariable_Wrap(out), Py_None, Py_None);
+  END_HANDLE_TH_ERRORS
+}
+
+// window_backward(q, k, v, out, lse, dout, window, sinks, scale, lens) -> (dq, dk, dv)
+PyObject* py_window_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *out, *lse, *dout, *lens;
+  linattn_window_desc x;
+  if (!tensor(a[0], q) || !tensor(a[1], k) || !tensor(a[2], v) || !tensor(a[3], out) || !tensor(a[4], lse) || !tensor(a[5], dout) || !tensor_or_none(a[9], lens) ||
+      !window_desc(*q, *k, *v, a[6], a[7], a[8], x) || !rows(*out, *q) || !rows(*dout, *q) || out->sizes() != q->sizes() || dout->sizes() != q->sizes() ||
+      !shaped(lse, at::kFloat, {q->size(0), q->size(1), q->size(2)}, *q) || !shaped(lens, at::kInt, {q->size(0)}, *q))
+    Py_RETURN_NONE;
+  void* s = nullptr;
+  bool other;
+  if (!stream_of(*q, s, other)) return nullptr;
+  if (other) Py_RETURN_NONE;
+  const int32_t L = (int32_t)q->size(2);
+  const at::Tensor dq = at::empty_like(*q), dk = at::empty_like(*k), dv = at::empty_like(*v);
+  x.out = strides(*out); x.dout = strides(*dout); x.dq = strides(dq); x.dk = strides(dk); x.dv = strides(dv);
+  const size_t bytes = lib.window_backward_workspace_bytes(&x, L);
+  const at::Tensor ws = scratch(bytes, *q);
+  const int st = without_gil(lib.window_backward, &x, L, ptr(q), ptr(k), ptr(v), ptr_as<int32_t>(lens), ptr(out), ptr_as<float>(lse), ptr(dout), ptr(&dq), ptr(&dk), ptr(&dv), ptr(some(ws)), bytes, s);
+  if (st != 0) return PyLong_FromLong(st);
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(dq), THPVariable_Wrap(dk), THPVariable_Wrap(dv));
+  END_HANDLE_TH_ERRORS
+}
+
+// window_step(q, k, v, (kcache, vcache, pos), window, sinks, scale, n_commit) -> out
+PyObject* py_window_step(PyObject*, PyObject* const* a, Py_ssize_t) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *kc, *vc, *pos, *n;
+  linattn_window_desc x;
+  if (!tensor(a[0], q) || !tensor(a[1], k) || !tensor(a[2], v) || !items(a[3], 3) || !tensor(PyTuple_GET_ITEM(a[3], 0), kc) || !tensor(PyTuple_GET_ITEM(a[3], 1), vc) ||
+      !tensor(PyTuple_GET_ITEM(a[3], 2), pos) || !tensor_or_none(a[7], n) || !window_desc(*q, *k, *v, a[4], a[5], a[6], x) || !q->is_contiguous() ||
+      !k->is_contiguous() || !v->is_contiguous())
+    Py_RETURN_NONE;
+  const int64_t B = x.B, Hkv = x.H_kv, held = (int64_t)x.sinks + x.window;
+  if (!shaped(kc, q->scalar_type(), {B, Hkv, held, x.d}, *q) || !shaped(vc, q->scalar_type(), {B, Hkv, held, x.d}, *q) || !shaped(pos, at::kInt, {B, Hkv}, *q) ||
+      !shaped(n, at::kInt, {B}, *q))
+    Py_RETURN_NONE;
+  void* s = nullptr;
+  bool other;
+  if (!stream_of(*q, s, other)) return nullptr;
+  if (other) Py_RETURN_NONE;
+  const int32_t kk = (int32_t)q->size(2);
+  const at::Tensor out = at::empty_like(*q);
+  const size_t bytes = lib.window_step_workspace_bytes(&x, kk);
+  const at::Tensor ws = scratch(bytes, *q);
+  const int st = without_gil(lib.window_step, &x, kk, ptr(q), ptr(k), ptr(v), ptr(kc), ptr(vc), ptr_as<int32_t>(pos), ptr_as<int32_t>(n), ptr(&out), ptr(some(ws)), bytes, s);
+  return out_or_status(st, out);
+  END_HANDLE_TH_ERRORS
+}
+
+// bind(the functions' addresses in the order of Library's members, _cuda_getDevice, _cuda_getCurrentRawStream)
 PyObject* py_bind(PyObject*, PyObject* args) {
-  unsigned long long p[9];
-  PyObject *dev, *raw;
-  if (!PyArg_ParseTuple(args, "KKKKKKKKKOO", p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8, &dev, &raw)) return nullptr;
-  auto set = [](auto& f, unsigned long long x) { f = reinterpret_cast<std::decay_t<decltype(f)>>(static_cast<uintptr_t>(x)); };
-  set(lib.workspace_bytes, p[0]); set(lib.prefill, p[1]); set(lib.prefill_grouped, p[2]);
-  set(lib.backward_workspace_bytes, p[3]); set(lib.prefill_grouped_backward, p[4]);
-  set(lib.verify, p[5]); set(lib.verify_grouped, p[6]); set(lib.verify_tree, p[7]); set(lib.decode, p[8]);
+  PyObject *addresses, *dev, *raw;
+  if (!PyArg_ParseTuple(args, "O!OO", &PyTuple_Type, &addresses, &dev, &raw)) return nullptr;
+  if (PyTuple_GET_SIZE(addresses) != kFunctions) {
+    PyErr_SetString(PyExc_ValueError, "bind: another number of functions");
+    return nullptr;
+  }
+  void* p[kFunctions];
+  for (int i = 0; i < kFunctions; ++i) {
+    p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  int i = 0;
+  auto set = [&](auto& f) { f = reinterpret_cast<std::decay_t<decltype(f)>>(p[i++]); };
+  set(lib.workspace_bytes); set(lib.prefill); set(lib.prefill_grouped); set(lib.backward_workspace_bytes); set(lib.prefill_grouped_backward);
+  set(lib.verify); set(lib.verify_grouped); set(lib.verify_tree); set(lib.decode);
+  set(lib.decay_workspace_bytes); set(lib.decay_prefill); set(lib.decay_backward_workspace_bytes); set(lib.decay_backward); set(lib.decay_step);
+  set(lib.window_prefill); set(lib.window_backward_workspace_bytes); set(lib.window_backward); set(lib.window_step_workspace_bytes); set(lib.window_step);
   Py_INCREF(dev);
   Py_INCREF(raw);
   Py_XSETREF(get_device, dev);
@@ -280,6 +510,8 @@ PyObject* py_bind(PyObject*, PyObject* args) {
 #define FAST(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("verify", py_verify), FAST("decode", py_decode), FAST("verify_tree", py_verify_tree),
                          FAST("verify_grouped", py_verify_grouped), FAST("prefill", py_prefill), FAST("prefill_grouped_backward", py_backward),
+                         FAST("decay_prefill", py_decay_prefill), FAST("decay_backward", py_decay_backward), FAST("decay_step", py_decay_step),
+                         FAST("window_prefill", py_window_prefill), FAST("window_backward", py_window_backward), FAST("window_step", py_window_step),
                          {"bind", py_bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
