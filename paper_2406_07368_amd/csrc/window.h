@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "decay.h"   // Rows, clamp_len
+#include "swizzle.h"
 
 namespace linattn {
 
@@ -15,8 +16,10 @@ struct WindowArgs {
   const int32_t* lens;
   float* lse;                     // [B,H,L]: written by the prefill (may be null), read by the gradient
   float* delta;                   // gradient: [B,H,L], dout . out
-  float* part;                    // gradient, far > 0: [B*H_kv][1 + 2 far][2][sinks][d], shares of the sinks' dk, dv
-  int far;                        // workgroups per key/value head for the queries that see nothing but sinks of key tile 0
+  int far;                        // gradient: workgroups per key/value head for the queries that see only sinks of key tile 0
+  int parts;                      // gradient: workgroups per key tile
+  float* sink_part;               // far > 0: [B*H_kv][parts + 2 far][2][sinks][d], shares of the sinks' dk, dv
+  float* part;                    // parts > 1: [B*H_kv][parts][2][L][d], shares of the other rows'
   int B, H, Hkv, L;
   int window, sinks;
   float scale;
@@ -71,8 +74,51 @@ __device__ __forceinline__ float max_xor32(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Consecutive workgroups go to the eight chiplets in turn, each with an L2 of its own: the places 0 .. n-1 of a launch
-// of 8 ceil(n / 8) workgroups so that a chiplet gets neighbours, which read the same keys.
-__device__ __forceinline__ int xcd_place(int block, int n) { return block % 8 * ((n + 7) / 8) + block / 8; }
+// Consecutive workgroups go to the eight chiplets in turn, each with an L2 of its own.  The `units` (a key/value head of a
+// batch row) of `each` workgroups, which read the same keys, are dealt out whole where every chiplet gets (nearly) as many;
+// else a chiplet takes a run of neighbours.  A launch has xcd_grid workgroups; a place >= units * each has no work.
+__host__ __device__ inline bool xcd_whole(int units) { return units % 8 == 0 || units >= 64; }
+__host__ __device__ inline int64_t xcd_grid(int units, int each) {
+  return xcd_whole(units) ? (int64_t)((units + 7) / 8) * 8 * each : ((int64_t)units * each + 7) / 8 * 8;
+}
+__device__ __forceinline__ int xcd_place(int block, int units, int each) {
+  const int x = block % 8, i = block / 8;
+  if (!xcd_whole(units)) return x * ((units * each + 7) / 8) + i;
+  const int u = x + 8 * (i / each);
+  return u < units ? u * each + i % each : units * each;
+}
+
+// 64 rows of D bf16 on their way from memory into LDS (swizzle.h): a thread's pieces.  `rows` of them are there; the others
+// re-read row 0 and become zeros.
+template <int D>
+struct Fetch {
+  static constexpr int PPR = D / 8, NP = 64 * PPR / 256;
+  u32x4 x[NP];
+  __device__ __forceinline__ void request(const uint16_t* row0, int64_t stride, int rows, int tid) {
+    const uint32_t st = (uint32_t)stride;                 // (at most 2^22: a tile's offsets fit 32 bits)
+    const uint32_t e = tid % PPR * 8, r = tid / PPR;
+    const char* base = reinterpret_cast<const char*>(row0);
+    if (rows >= 64) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) x[i] = *reinterpret_cast<const u32x4*>(base + ((r + 256 / PPR * i) * st + e) * 2);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const uint32_t ri = r + 256 / PPR * i;
+        x[i] = *reinterpret_cast<const u32x4*>(base + ((ri < (uint32_t)rows ? ri : 0) * st + e) * 2);
+      }
+    }
+  }
+  __device__ __forceinline__ void put(uint16_t* lds, int rows, int tid) {
+    uint16_t* d = lds + Swizzled<D>::piece(tid / PPR, tid % PPR);   // (the pieces' rows are the same modulo 16)
+    if (rows < 64) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        if (tid / PPR + 256 / PPR * i >= rows) x[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) *reinterpret_cast<u32x4*>(d + 256 / PPR * i * D) = x[i];
+  }
+};
 
 }  // namespace linattn

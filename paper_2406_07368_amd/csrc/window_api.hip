@@ -49,21 +49,27 @@ WindowArgs args(const linattn_window_desc* d, int32_t L, const void* q, const vo
 }
 
 struct GradientPlan {
-  int far;                                        // see WindowArgs
-  size_t off_part, bytes;
+  int far, parts;                                 // see WindowArgs
+  size_t off_sinks, off_part, bytes;
 };
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 GradientPlan plan_gradient(const linattn_window_desc* d, int32_t L) {
   GradientPlan p{};
-  const int64_t heads = (int64_t)d->B * d->H_kv;
-  const int tiles = (L + kWindowQ - 1) / kWindowQ, far_tiles = tiles - window_far_tile(d->window);
-  if (d->sinks > 0 && far_tiles > 0) {
-    const int64_t items = (int64_t)far_tiles * (d->H / d->H_kv);
-    int64_t n = (512 + heads - 1) / heads;        // workgroups enough to fill the chip, four query tiles each or more
+  const int64_t heads = (int64_t)d->B * d->H_kv, group = d->H / d->H_kv;
+  const int tiles = (L + kWindowQ - 1) / kWindowQ, near = window_far_tile(d->window) < tiles ? window_far_tile(d->window) : tiles;
+  // few key tiles: as many workgroups for each as the chip has room for, with four query tiles each or more
+  const int64_t wgs = heads * ((L + kWindowKeys - 1) / kWindowKeys);
+  int64_t parts = 256 / wgs < near * group / 4 ? 256 / wgs : near * group / 4;
+  p.parts = parts < 1 ? 1 : (int)parts;
+  if (d->sinks > 0 && tiles > near) {
+    const int64_t items = (int64_t)(tiles - near) * group;
+    int64_t n = (512 + heads - 1) / heads;
     if (n > (items + 3) / 4) n = (items + 3) / 4;
     p.far = (int)n;
   }
-  p.off_part = ((size_t)d->B * d->H * L * sizeof(float) + 255) / 256 * 256;
-  p.bytes = p.off_part + (p.far ? (size_t)heads * (1 + 2 * p.far) * 2 * d->sinks * d->d * sizeof(float) : 0);
+  p.off_sinks = round256((size_t)d->B * d->H * L * sizeof(float));
+  p.off_part = p.off_sinks + round256(p.far ? (size_t)heads * (p.parts + 2 * p.far) * 2 * d->sinks * d->d * sizeof(float) : 0);
+  p.bytes = p.off_part + (p.parts > 1 ? (size_t)heads * p.parts * 2 * L * d->d * sizeof(float) : 0);
   return p;
 }
 
@@ -117,8 +123,9 @@ linattn_status linattn_window_backward(const linattn_window_desc* desc, int32_t 
   a.dq = rows(dq, desc->dq); a.dk = rows(dk, desc->dk); a.dv = rows(dv, desc->dv);
   a.lse = const_cast<float*>(lse);
   a.delta = static_cast<float*>(workspace);
+  a.sink_part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_sinks);
   a.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
-  a.far = p.far;
+  a.far = p.far; a.parts = p.parts;
   return launch_window_backward(a, desc->d, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? LINATTN_OK : LINATTN_ERR_HIP;
 }
 

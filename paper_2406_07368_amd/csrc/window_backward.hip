@@ -11,8 +11,8 @@
 //   rows of k, v 128 keys of a key/value head a workgroup, a wave's 32 in its lanes, queries 64 at a time through LDS,
 //                over all query heads that share the keys: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
 // Key tile 0 would meet every query of the sequence for the sake of its sinks, many times what other tiles have to do: the
-// query tiles that see nothing of it but sinks are shared out over workgroups of their own, whose sums (fp32, per wave)
-// go to the workspace and are added up in a fixed order by a third launch.
+// query tiles that see nothing of it but sinks are shared out over workgroups of their own, and where there are few key
+// tiles each is shared by several workgroups.  Their sums (fp32) go to the workspace and are added up in a fixed order.
 //
 // Bound: the matrix cores (14 d flops a visible pair here).
 #include "common.h"
@@ -26,14 +26,12 @@ namespace {
 
 template <int D>
 struct Cfg {
-  static constexpr int RS = D + 16;
-  static constexpr int BUF = 2 * 64 * RS;       // elements of one buffer: 64 rows of two tensors
-  static constexpr int BYTES = 2 * BUF * 2 + 4 * 64 * 4;   // ... and (rows of k, v) lse and delta, two buffers
+  static constexpr int BUF = 2 * 64 * D;        // elements of one buffer: 64 rows of two tensors
   static constexpr int OS = D + 8;
+  static constexpr int TILES = (2 * BUF > 128 * OS ? 2 * BUF : 128 * OS) * 2;   // bytes: the buffers; finished rows
+  static constexpr int BYTES = TILES + 4 * 64 * 4;   // ... and (rows of k, v) lse and delta, two buffers
   static constexpr int PPR = D / 8;
-  static constexpr int NP = 64 * PPR / 256;
   static constexpr int CT = D / 32, KS = D / 16;
-  static_assert(128 * OS <= 2 * BUF, "the finished rows take the buffers' place");
 };
 
 // 128 finished rows, X^T in accumulators (a row per lane of each wave, its elements in the registers) -> whole rows
@@ -65,16 +63,16 @@ __device__ __forceinline__ void zero_rows(uint16_t* out, int64_t st, int r0, int
 }
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, int n) {
+__global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
-  const int place = xcd_place(blockIdx.x, n);
-  if (place >= n) return;
+  const int group = a.H / a.Hkv, ntile = (a.L + 127) / 128;
+  const int place = xcd_place(blockIdx.x, a.B * a.Hkv, group * ntile);
+  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
+  if (bk >= a.B * a.Hkv) return;
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int group = a.H / a.Hkv, ntile = (a.L + 127) / 128;
-  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
   const int b = bk / a.Hkv, hk = bk % a.Hkv, h = hk * group + g;
   const int len = clamp_len(a.lens, b, a.L);
   const int t0 = tile * 128, t_end = t0 + 128 < a.L ? t0 + 128 : a.L;
@@ -87,6 +85,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, int n) 
   const uint16_t* gk = static_cast<const uint16_t*>(a.k.p) + b * a.k.b + hk * a.k.h;
   const uint16_t* gv = static_cast<const uint16_t*>(a.v.p) + b * a.v.b + hk * a.v.h;
   const float c = window_log2_scale(a.scale);
+  const Swizzled<D> lds(lane, 4);
   const int t = t0 + 32 * w + l32, tw = t0 + 32 * w, tr = t < len ? t : len - 1;
   bf16x8 qop[G::KS], dop[G::KS];
   float delta = 0.f;
@@ -112,46 +111,31 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, int n) 
   const int ns = a.sinks > 0 && lo > 0 ? 1 : 0;
   const int nk = ns + last / 64 - lo + 1;
   auto key0 = [&](int i) { return (i < ns ? i : lo + i - ns) * 64; };
-  u32x4 rk[G::NP], rv[G::NP];
-  auto request = [&](int s0) {
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i, s = s0 + p / G::PPR, e = p % G::PPR * 8;
-      const int row = s < len ? s : 0;
-      rk[i] = *reinterpret_cast<const u32x4*>(gk + row * a.k.t + e);
-      rv[i] = *reinterpret_cast<const u32x4*>(gv + row * a.v.t + e);
-    }
+  Fetch<D> fk, fv;
+  auto request = [&](int i) {
+    const int s0 = key0(i);
+    fk.request(gk + s0 * a.k.t, a.k.t, len - s0, tid);
+    fv.request(gv + s0 * a.v.t, a.v.t, len - s0, tid);
   };
-  auto put = [&](int s0, uint16_t* buf) {
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i;
-      uint16_t* d = buf + p / G::PPR * G::RS + p % G::PPR * 8;
-      const u32x4 z = {0u, 0u, 0u, 0u};
-      const bool in = s0 + p / G::PPR < len;
-      *reinterpret_cast<u32x4*>(d) = in ? rk[i] : z;
-      *reinterpret_cast<u32x4*>(d + 64 * G::RS) = in ? rv[i] : z;
-    }
+  auto put = [&](int i, uint16_t* buf) {
+    const int n = len - key0(i);
+    fk.put(buf, n, tid);
+    fv.put(buf + 64 * D, n, tid);
   };
   f32x16 dQ[G::CT];
 #pragma unroll
   for (int i = 0; i < G::CT; ++i) dQ[i] = f32x16{};
-  request(key0(0));
-  put(key0(0), smem);
-  for (int i = 0; i < nk; ++i) {
-    const int s0 = key0(i);
-    const uint16_t *Kl = smem + (i & 1) * G::BUF, *Vl = Kl + 64 * G::RS;
-    __syncthreads();
-    if (i + 1 < nk) request(key0(i + 1));
+  auto tile_of = [&](int i, const uint16_t* Kl) {
+    const uint16_t* Vl = Kl + 64 * D;
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const int sw = s0 + 32 * kt;
+      const int sw = key0(i) + 32 * kt;
       if (!(sw <= tw + 31 && (sw + 31 > tw - a.window || sw < a.sinks))) continue;
       f32x16 x = {}, y = {};
 #pragma unroll
       for (int ks = 0; ks < G::KS; ++ks) {
-        x = mfma(lds_row8(Kl + (32 * kt + l32) * G::RS + 16 * ks + 8 * hi), qop[ks], x);
-        y = mfma(lds_row8(Vl + (32 * kt + l32) * G::RS + 16 * ks + 8 * hi), dop[ks], y);
+        x = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x);
+        y = mfma(lds.rows(Vl, 32 * kt, ks), dop[ks], y);
       }
       const bool all = sw + 31 <= tw && (sw > tw + 31 - a.window || sw + 32 <= a.sinks);
 #pragma unroll
@@ -165,39 +149,60 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, int n) 
       for (int half = 0; half < 2; ++half) {
         const bf16x8 p = pack8(x, 8 * half);
 #pragma unroll
-        for (int ct = 0; ct < G::CT; ++ct) dQ[ct] = mfma(tr_operand_acc_order(Kl, G::RS, 32 * kt + 16 * half, 32 * ct, lane), p, dQ[ct]);
+        for (int ct = 0; ct < G::CT; ++ct) dQ[ct] = mfma(lds.cols_acc(Kl, 32 * kt + 16 * half, ct), p, dQ[ct]);
       }
     }
-    if (i + 1 < nk) put(key0(i + 1), smem + ((i + 1) & 1) * G::BUF);
+  };
+  uint16_t *even = smem, *odd = smem + G::BUF;
+  request(0);
+  put(0, even);
+  for (int i = 0; i < nk; i += 2) {
+    __syncthreads();
+    if (i + 1 < nk) request(i + 1);
+    tile_of(i, even);
+    if (i + 1 >= nk) break;
+    put(i + 1, odd);
+    __syncthreads();
+    if (i + 2 < nk) request(i + 2);
+    tile_of(i + 1, odd);
+    if (i + 2 < nk) put(i + 2, even);
   }
   store_tile<D>(smem, dQ, a.scale, gdq, a.dq.t, t0, t_end, len, tid);
 }
 
-// SINKS: the query tiles beyond window_far_tile of key tile 0; the waves take (32 keys, 32 queries) each.
-template <int D, bool SINKS>
-__global__ __launch_bounds__(256, 1) void window_dkv_kernel(WindowArgs a, int n) {
+// Jobs of a key/value head: `far` for the sinks (the query tiles from window_far_tile on, with the sinks of key tile 0; the
+// waves take 32 keys and 32 queries of a tile each), then `parts` for every key tile.
+template <int D>
+__global__ __launch_bounds__(256, 1) void window_dkv_kernel(WindowArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
-  float* stats = reinterpret_cast<float*>(smem + 2 * G::BUF);    // [2][lse | delta][64]
-  const int place = SINKS ? (int)blockIdx.x : xcd_place(blockIdx.x, n);
-  if (place >= n) return;
+  float* stats = reinterpret_cast<float*>(smem + G::TILES / 2);    // [2][lse | delta][64]
+  const int group = a.H / a.Hkv, each = a.far + a.parts * ((a.L + 127) / 128);
+  const int place = xcd_place(blockIdx.x, a.B * a.Hkv, each);
+  const int bk = place / each;
+  if (bk >= a.B * a.Hkv) return;
+  const bool sink_job = place % each < a.far;
+  const int tile = sink_job ? 0 : (place % each - a.far) / a.parts;
+  const int part = sink_job ? place % each : (place % each - a.far) % a.parts;
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int group = a.H / a.Hkv, ntile = SINKS ? a.far : (a.L + 127) / 128;
-  const int tile = place % ntile, bk = place / ntile;
   const int b = bk / a.Hkv, hk = bk % a.Hkv;
   const int len = clamp_len(a.lens, b, a.L);
-  const int s0 = SINKS ? 0 : tile * 128, s_end = s0 + 128 < a.L ? s0 + 128 : a.L;
+  const int s0 = tile * 128, s_end = s0 + 128 < a.L ? s0 + 128 : a.L;
   uint16_t* gdk = const_cast<uint16_t*>(static_cast<const uint16_t*>(a.dk.p)) + b * a.dk.b + hk * a.dk.h;
   uint16_t* gdv = const_cast<uint16_t*>(static_cast<const uint16_t*>(a.dv.p)) + b * a.dv.b + hk * a.dv.h;
-  if (!SINKS && s0 >= len && !(a.far > 0 && s0 == 0)) {
-    zero_rows<D>(gdk, a.dk.t, s0, s_end, tid);
-    zero_rows<D>(gdv, a.dv.t, s0, s_end, tid);
+  const bool shares = a.far > 0 && s0 == 0;                      // the sinks' rows are added up from shares
+  if (s0 >= len && !shares) {
+    if (part == 0) {
+      zero_rows<D>(gdk, a.dk.t, s0, s_end, tid);
+      zero_rows<D>(gdv, a.dv.t, s0, s_end, tid);
+    }
     return;
   }
   const float c = window_log2_scale(a.scale);
-  const int kw = SINKS ? 32 * (w & 1) : s0 + 32 * w;             // the wave's first key
+  const Swizzled<D> lds(lane, 4);
+  const int kw = sink_job ? 32 * (w & 1) : s0 + 32 * w;          // the wave's first key
   const int s = kw + l32;                                        // this lane's key
   bf16x8 kop[G::KS], vop[G::KS];
   {
@@ -210,78 +215,49 @@ __global__ __launch_bounds__(256, 1) void window_dkv_kernel(WindowArgs a, int n)
       vop[ks] = *reinterpret_cast<const bf16x8*>(pv + 16 * ks);
     }
   }
-  // query tiles of one head: q_lo .. q_hi - 1; this workgroup's items are (head of the group, tile)
+  // query tiles of one head: q_lo .. q_lo + q_n - 1; the items are (head of the group, tile), every step-th of them this workgroup's
   const int q_len = (len + 63) / 64;
-  const int far0 = window_far_tile(a.window);
-  int q_lo, q_n, first, step;
-  if (SINKS) {
-    q_lo = far0; q_n = q_len > far0 ? q_len - far0 : 0;
-    first = tile; step = a.far;
-  } else {
-    q_lo = s0 / 64;
-    const int64_t end = ((int64_t)s0 + 127 + a.window - 1) / 64 + 1;   // (key tile 0: window_far_tile)
-    q_n = q_len < end ? q_len - q_lo : (int)end - q_lo;
-    if (q_n < 0) q_n = 0;
-    first = 0; step = 1;
-  }
+  const int64_t near_end = ((int64_t)s0 + 127 + a.window - 1) / 64 + 1;   // (key tile 0: window_far_tile)
+  const int end = q_len < near_end ? q_len : (int)near_end;
+  const int q_lo = sink_job ? end : s0 / 64;
+  const int q_n = (sink_job ? q_len : end) - q_lo > 0 ? (sink_job ? q_len : end) - q_lo : 0;
+  const int step = sink_job ? a.far : a.parts;
   const int items = q_n * group;
 
-  u32x4 rq[G::NP], rd[G::NP];
+  Fetch<D> fq, fd;
   float rs = 0.f;
+  auto first_row = [&](int it) { return (q_lo + it % q_n) * 64; };
   auto request = [&](int it) {
-    const int h = hk * group + it / q_n, t0 = (q_lo + it % q_n) * 64;
-    const uint16_t* gq = static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h;
-    const uint16_t* gd = static_cast<const uint16_t*>(a.dout.p) + b * a.dout.b + h * a.dout.h;
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i, t = t0 + p / G::PPR, e = p % G::PPR * 8;
-      const int row = t < len ? t : 0;
-      rq[i] = *reinterpret_cast<const u32x4*>(gq + row * a.q.t + e);
-      rd[i] = *reinterpret_cast<const u32x4*>(gd + row * a.dout.t + e);
-    }
+    const int h = hk * group + it / q_n, t0 = first_row(it), n = len - t0;
+    fq.request(static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h + t0 * a.q.t, a.q.t, n, tid);
+    fd.request(static_cast<const uint16_t*>(a.dout.p) + b * a.dout.b + h * a.dout.h + t0 * a.dout.t, a.dout.t, n, tid);
     if (tid < 128) {
-      const int t = t0 + (tid & 63);
-      const int64_t at = ((int64_t)b * a.H + h) * a.L + t;
-      rs = t < len ? (tid < 64 ? a.lse[at] * 1.44269504088896340736f : a.delta[at]) : 0.f;
+      const int64_t at = ((int64_t)b * a.H + h) * a.L + t0 + (tid & 63);
+      rs = (tid & 63) < n ? (tid < 64 ? a.lse[at] * 1.44269504088896340736f : a.delta[at]) : 0.f;
     }
   };
-  auto put = [&](int it, int which) {
-    const int t0 = (q_lo + it % q_n) * 64;
-    uint16_t* buf = smem + which * G::BUF;
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i;
-      uint16_t* d = buf + p / G::PPR * G::RS + p % G::PPR * 8;
-      const u32x4 z = {0u, 0u, 0u, 0u};
-      const bool in = t0 + p / G::PPR < len;
-      *reinterpret_cast<u32x4*>(d) = in ? rq[i] : z;
-      *reinterpret_cast<u32x4*>(d + 64 * G::RS) = in ? rd[i] : z;
-    }
-    if (tid < 128) stats[which * 128 + tid] = rs;
+  auto put = [&](int it, uint16_t* buf, float* st) {
+    const int n = len - first_row(it);
+    fq.put(buf, n, tid);
+    fd.put(buf + 64 * D, n, tid);
+    if (tid < 128) st[tid] = rs;
   };
 
   f32x16 dK[G::CT], dV[G::CT];
 #pragma unroll
   for (int i = 0; i < G::CT; ++i) { dK[i] = f32x16{}; dV[i] = f32x16{}; }
-  if (first < items) {
-    request(first);
-    put(first, 0);
-  }
-  for (int it = first, par = 0; it < items; it += step, par ^= 1) {
-    const int t0 = (q_lo + it % q_n) * 64;
-    const uint16_t *Ql = smem + par * G::BUF, *dl = Ql + 64 * G::RS;
-    const float* st = stats + par * 128;
-    __syncthreads();
-    if (it + step < items) request(it + step);
+  auto tile_of = [&](int it, const uint16_t* Ql, const float* st) {
+    const uint16_t* dl = Ql + 64 * D;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      const int tw = t0 + 32 * tt;
-      if (SINKS ? (tt != w >> 1 || kw >= a.sinks || tw >= len) : !(kw <= tw + 31 && (kw + 31 > tw - a.window || kw < a.sinks) && tw < len)) continue;
+      const int tw = first_row(it) + 32 * tt;
+      if (tw >= len) continue;
+      if (sink_job ? tt != w >> 1 || kw >= a.sinks : !(kw <= tw + 31 && (kw + 31 > tw - a.window || kw < a.sinks))) continue;
       f32x16 x = {}, y = {};
 #pragma unroll
       for (int ks = 0; ks < G::KS; ++ks) {
-        x = mfma(lds_row8(Ql + (32 * tt + l32) * G::RS + 16 * ks + 8 * hi), kop[ks], x);
-        y = mfma(lds_row8(dl + (32 * tt + l32) * G::RS + 16 * ks + 8 * hi), vop[ks], y);
+        x = mfma(lds.rows(Ql, 32 * tt, ks), kop[ks], x);
+        y = mfma(lds.rows(dl, 32 * tt, ks), vop[ks], y);
       }
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
@@ -306,67 +282,100 @@ __global__ __launch_bounds__(256, 1) void window_dkv_kernel(WindowArgs a, int n)
         const bf16x8 p = pack8(x, 8 * half), ds = pack8(y, 8 * half);
 #pragma unroll
         for (int ct = 0; ct < G::CT; ++ct) {
-          dV[ct] = mfma(tr_operand_acc_order(dl, G::RS, 32 * tt + 16 * half, 32 * ct, lane), p, dV[ct]);
-          dK[ct] = mfma(tr_operand_acc_order(Ql, G::RS, 32 * tt + 16 * half, 32 * ct, lane), ds, dK[ct]);
+          dV[ct] = mfma(lds.cols_acc(dl, 32 * tt + 16 * half, ct), p, dV[ct]);
+          dK[ct] = mfma(lds.cols_acc(Ql, 32 * tt + 16 * half, ct), ds, dK[ct]);
         }
       }
     }
-    if (it + step < items) put(it + step, par ^ 1);
+  };
+  uint16_t *even = smem, *odd = smem + G::BUF;
+  if (part < items) {
+    request(part);
+    put(part, even, stats);
   }
-  if (!SINKS) {
+  for (int it = part; it < items; it += 2 * step) {
+    __syncthreads();
+    if (it + step < items) request(it + step);
+    tile_of(it, even, stats);
+    if (it + step >= items) break;
+    put(it + step, odd, stats + 128);
+    __syncthreads();
+    if (it + 2 * step < items) request(it + 2 * step);
+    tile_of(it + step, odd, stats + 128);
+    if (it + 2 * step < items) put(it + 2 * step, even, stats);
+  }
+  if (!sink_job && a.parts == 1) {
     store_tile<D>(smem, dK, a.scale, gdk, a.dk.t, s0, s_end, len, tid);
     store_tile<D>(smem, dV, 1.f, gdv, a.dv.t, s0, s_end, len, tid);
   }
-  // the sinks' shares: slot 0 what key tile 0 met in its own query tiles, then a slot for each wave half of each SINKS workgroup
-  if (a.far > 0 && s0 == 0 && s < a.sinks) {
-    const int slot = SINKS ? 1 + 2 * tile + (w >> 1) : 0;
-    float* p = a.part + (((int64_t)bk * (1 + 2 * a.far) + slot) * 2 * a.sinks + s) * D;
+  // where the sums of this lane's key go, if they are a share: [2][rows][D], dk then dv
+  auto give = [&](float* p, int64_t rows) {
 #pragma unroll
     for (int ct = 0; ct < G::CT; ++ct)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const int e = 32 * ct + 8 * r4 + 4 * hi;
         *reinterpret_cast<f32x4*>(p + e) = f32x4{dK[ct][4 * r4], dK[ct][4 * r4 + 1], dK[ct][4 * r4 + 2], dK[ct][4 * r4 + 3]};
-        *reinterpret_cast<f32x4*>(p + (int64_t)a.sinks * D + e) = f32x4{dV[ct][4 * r4], dV[ct][4 * r4 + 1], dV[ct][4 * r4 + 2], dV[ct][4 * r4 + 3]};
+        *reinterpret_cast<f32x4*>(p + rows * D + e) = f32x4{dV[ct][4 * r4], dV[ct][4 * r4 + 1], dV[ct][4 * r4 + 2], dV[ct][4 * r4 + 3]};
       }
+  };
+  if (shares && s < a.sinks) {
+    const int slot = sink_job ? a.parts + 2 * part + (w >> 1) : part;
+    give(a.sink_part + (((int64_t)bk * (a.parts + 2 * a.far) + slot) * 2 * a.sinks + s) * D, a.sinks);
+  } else if (!sink_job && a.parts > 1 && s < s_end) {
+    give(a.part + (((int64_t)bk * a.parts + part) * 2 * a.L + s) * D, a.L);
   }
 }
 
-// a sink row's gradient: the sum of its shares, a wave per row of dk or dv
-template <int D>
-__global__ __launch_bounds__(64) void window_sinks_kernel(WindowArgs a) {
-  const int s = blockIdx.x % a.sinks, kv = blockIdx.x / a.sinks % 2, bk = blockIdx.x / (2 * a.sinks);
-  const int b = bk / a.Hkv, hk = bk % a.Hkv, slots = 1 + 2 * a.far;
-  const Rows& o = kv ? a.dv : a.dk;
-  uint16_t* out = const_cast<uint16_t*>(static_cast<const uint16_t*>(o.p)) + b * o.b + hk * o.h + s * o.t;
-  const bool in = s < clamp_len(a.lens, b, a.L);
-  for (int e = threadIdx.x; e < D; e += 64) {
-    const float* p = a.part + (((int64_t)bk * slots * 2 + kv) * a.sinks + s) * D + e;
-    float x = 0.f;
-    for (int i = 0; i < slots; ++i) x += p[(int64_t)i * 2 * a.sinks * D];
-    out[e] = in ? f32_to_bf16_bits(kv ? x : x * a.scale) : 0;
+// Gradient rows of k or v from their `slots` shares [bk][slot][2][n_rows][D].  SINKS: a sink's row a workgroup, its shares
+// dealt out over the threads; else several rows, all but the sinks' if these have shares of their own.
+template <int D, bool SINKS>
+__global__ __launch_bounds__(256) void window_shares_kernel(WindowArgs a) {
+  constexpr int LR = D / 4, PER = 256 / LR;      // threads of a row; rows (or slots) at a time
+  __shared__ __attribute__((aligned(16))) float sum[PER][D];
+  const int kv = blockIdx.x & 1, bk = blockIdx.x >> 1, b = bk / a.Hkv, hk = bk % a.Hkv;
+  const int e = threadIdx.x % LR * 4, u = threadIdx.x / LR;
+  const int n_rows = SINKS ? a.sinks : a.L, slots = SINKS ? a.parts + 2 * a.far : a.parts;
+  const int row = SINKS ? blockIdx.y : blockIdx.y * PER + u;
+  const int len = clamp_len(a.lens, b, a.L);
+  if (!SINKS && (row >= a.L || (a.far > 0 && row < a.sinks))) return;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (row < len) {
+    const float* p = (SINKS ? a.sink_part : a.part) + (((int64_t)bk * slots * 2 + kv) * n_rows + row) * D + e;
+#pragma unroll 4
+    for (int i = SINKS ? u : 0; i < slots; i += SINKS ? PER : 1) x += *reinterpret_cast<const f32x4*>(p + (int64_t)i * 2 * n_rows * D);
   }
+  if (SINKS) {
+    *reinterpret_cast<f32x4*>(&sum[u][e]) = x;
+    __syncthreads();
+    if (u > 0) return;
+#pragma unroll
+    for (int i = 1; i < PER; ++i) x += *reinterpret_cast<const f32x4*>(&sum[i][e]);
+  }
+  if (!kv) x *= a.scale;
+  const Rows& o = kv ? a.dv : a.dk;
+  uint16_t* out = const_cast<uint16_t*>(static_cast<const uint16_t*>(o.p)) + b * o.b + hk * o.h + row * o.t;
+  *reinterpret_cast<u32x2*>(out + e) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
 }
 
 template <int D>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  const int nq = a.B * a.H * ((a.L + 127) / 128), nk = a.B * a.Hkv * ((a.L + 127) / 128);
+  const int heads = a.B * a.Hkv, tiles = (a.L + 127) / 128;
   hipError_t e = LINATTN_MAX_LDS_ONCE((window_dq_kernel<D>), Cfg<D>::BYTES);
   if (e != hipSuccess) return e;
-  e = LINATTN_MAX_LDS_ONCE((window_dkv_kernel<D, false>), Cfg<D>::BYTES);
+  e = LINATTN_MAX_LDS_ONCE((window_dkv_kernel<D>), Cfg<D>::BYTES);
   if (e != hipSuccess) return e;
-  window_dq_kernel<D><<<dim3((nq + 7) / 8 * 8), 256, Cfg<D>::BYTES, s>>>(a, nq);
+  window_dq_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.H / a.Hkv * tiles)), 256, Cfg<D>::BYTES, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.far > 0) {
-    e = LINATTN_MAX_LDS_ONCE((window_dkv_kernel<D, true>), Cfg<D>::BYTES);
-    if (e != hipSuccess) return e;
-    window_dkv_kernel<D, true><<<dim3(a.B * a.Hkv * a.far), 256, Cfg<D>::BYTES, s>>>(a, a.B * a.Hkv * a.far);
+  window_dkv_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.far + a.parts * tiles)), 256, Cfg<D>::BYTES, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.parts > 1) {
+    constexpr int PER = 1024 / D;
+    window_shares_kernel<D, false><<<dim3(2 * heads, (a.L + PER - 1) / PER), 256, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  window_dkv_kernel<D, false><<<dim3((nk + 7) / 8 * 8), 256, Cfg<D>::BYTES, s>>>(a, nk);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.far > 0) {
-    window_sinks_kernel<D><<<dim3(a.B * a.Hkv * 2 * a.sinks), 64, 0, s>>>(a);
+    window_shares_kernel<D, true><<<dim3(2 * heads, a.sinks), 256, 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;

@@ -21,29 +21,28 @@ namespace {
 
 constexpr int QT = 128, KT = 64;
 
+constexpr float kLate = 8.f;   // log2: how far a running maximum may lie behind before the sums are scaled anew
+
 template <int D>
 struct Cfg {
-  static constexpr int RS = D + 16;
-  static constexpr int BUF = 2 * KT * RS;       // elements: K, V
-  static constexpr int BYTES = 2 * BUF * 2;
+  static constexpr int BUF = 2 * KT * D;        // elements: K, V
   static constexpr int OS = D + 8;              // finished rows
+  static constexpr int BYTES = (2 * BUF > QT * OS ? 2 * BUF : QT * OS) * 2;
   static constexpr int PPR = D / 8;
-  static constexpr int NP = KT * PPR / 256;
-  static_assert(QT * OS <= 2 * BUF, "the finished rows take the buffers' place");
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a, int n) {
+__global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
-  const int place = xcd_place(blockIdx.x, n);
-  if (place >= n) return;
+  // the query heads that share keys side by side, then the query tiles
+  const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
+  const int place = xcd_place(blockIdx.x, a.B * a.Hkv, group * ntile);
+  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
+  if (bk >= a.B * a.Hkv) return;
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  // the query heads that share keys side by side, then the query tiles
-  const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
-  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
   const int b = bk / a.Hkv, hk = bk % a.Hkv, h = hk * group + g;
   const int len = clamp_len(a.lens, b, a.L);
   const int t0 = tile * QT, t_end = t0 + QT < a.L ? t0 + QT : a.L;
@@ -62,6 +61,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a, in
   const uint16_t* gk = static_cast<const uint16_t*>(a.k.p) + b * a.k.b + hk * a.k.h;
   const uint16_t* gv = static_cast<const uint16_t*>(a.v.p) + b * a.v.b + hk * a.v.h;
   const float c = window_log2_scale(a.scale);
+  const Swizzled<D> lds(lane, 4);
 
   const int t = t0 + 32 * w + l32;              // this lane's query
   const int tw = t0 + 32 * w;                   // the wave's first
@@ -78,26 +78,16 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a, in
   const int nk = ns + last / KT - lo + 1;
   auto key0 = [&](int i) { return (i < ns ? i : lo + i - ns) * KT; };
 
-  u32x4 rk[G::NP], rv[G::NP];
-  auto request = [&](int s0) {
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i, s = s0 + p / G::PPR, e = p % G::PPR * 8;
-      const int row = s < len ? s : 0;
-      rk[i] = *reinterpret_cast<const u32x4*>(gk + row * a.k.t + e);
-      rv[i] = *reinterpret_cast<const u32x4*>(gv + row * a.v.t + e);
-    }
+  Fetch<D> fk, fv;
+  auto request = [&](int i) {
+    const int s0 = key0(i);
+    fk.request(gk + s0 * a.k.t, a.k.t, len - s0, tid);
+    fv.request(gv + s0 * a.v.t, a.v.t, len - s0, tid);
   };
-  auto put = [&](int s0, uint16_t* buf) {
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i;
-      uint16_t* d = buf + p / G::PPR * G::RS + p % G::PPR * 8;
-      const u32x4 z = {0u, 0u, 0u, 0u};
-      const bool in = s0 + p / G::PPR < len;
-      *reinterpret_cast<u32x4*>(d) = in ? rk[i] : z;
-      *reinterpret_cast<u32x4*>(d + KT * G::RS) = in ? rv[i] : z;
-    }
+  auto put = [&](int i, uint16_t* buf) {
+    const int n = len - key0(i);
+    fk.put(buf, n, tid);
+    fv.put(buf + KT * D, n, tid);
   };
 
   f32x16 O[D / 32];
@@ -105,60 +95,65 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a, in
   for (int i = 0; i < D / 32; ++i) O[i] = f32x16{};
   float m = -__builtin_inff(), l = 0.f;         // l: this lane's half of the keys
 
-  request(key0(0));
-  put(key0(0), smem);
-  for (int i = 0; i < nk; ++i) {
+  auto tile_of = [&](int i, const uint16_t* Kl) {
+    const uint16_t* Vl = Kl + KT * D;
     const int s0 = key0(i);
-    const uint16_t *Kl = smem + (i & 1) * G::BUF, *Vl = Kl + KT * G::RS;
-    __syncthreads();
-    if (i + 1 < nk) request(key0(i + 1));
-    const bool some = s0 <= tw + 31 && (s0 + KT - 1 > tw - a.window || s0 < a.sinks);
-    if (some) {
-      f32x16 x[2] = {};
+    if (!(s0 <= tw + 31 && (s0 + KT - 1 > tw - a.window || s0 < a.sinks))) return;
+    f32x16 x[2] = {};
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) x[kt] = mfma(lds_row8(Kl + (32 * kt + l32) * G::RS + 16 * ks + 8 * hi), qop[ks], x[kt]);
-      const bool all = s0 + KT - 1 <= tw && (s0 > tw + 31 - a.window || s0 + KT <= a.sinks);
-      if (!all) {
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!window_sees(t, s0 + 32 * kt + acc_row(r, hi), a.window, a.sinks)) x[kt][r] = -__builtin_inff();
-      }
-      float top = x[0][0];
+      for (int ks = 0; ks < D / 16; ++ks) x[kt] = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x[kt]);
+    const bool all = s0 + KT - 1 <= tw && (s0 > tw + 31 - a.window || s0 + KT <= a.sinks);
+    if (!all) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, x[kt][r]);
-      const float m2 = fmaxf(m, max_xor32(top) * c);
-      const float mm = m2 == -__builtin_inff() ? 0.f : m2;     // nothing seen yet: every weight is exp2(-inf)
-      const float f = __builtin_amdgcn_exp2f(m - mm);
-      m = m2;
-      float sum = 0.f;
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          x[kt][r] = __builtin_amdgcn_exp2f(x[kt][r] * c - mm);
-          sum += x[kt][r];
-        }
-      l = l * f + sum;
-      if (__any(f != 1.f)) {
-#pragma unroll
-        for (int ct = 0; ct < D / 32; ++ct) O[ct] *= f;
-      }
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const bf16x8 p = pack8(x[kt], 8 * half);
-#pragma unroll
-          for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(tr_operand_acc_order(Vl, G::RS, 32 * kt + 16 * half, 32 * ct, lane), p, O[ct]);
-        }
+        for (int r = 0; r < 16; ++r)
+          if (!window_sees(t, s0 + 32 * kt + acc_row(r, hi), a.window, a.sinks)) x[kt][r] = -__builtin_inff();
     }
-    if (i + 1 < nk) put(key0(i + 1), smem + ((i + 1) & 1) * G::BUF);
+    float top = x[0][0];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, x[kt][r]);
+    top = max_xor32(top) * c;
+    if (__any(top > m + kLate)) {
+      const float m2 = fmaxf(m, top);
+      const float f = m2 == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= f;
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct) O[ct] *= f;
+    }
+    const float mm = m == -__builtin_inff() ? 0.f : m;         // nothing seen yet: every weight is exp2(-inf)
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int r = 8 * half; r < 8 * half + 8; ++r) {
+          x[kt][r] = __builtin_amdgcn_exp2f(x[kt][r] * c - mm);
+          l += x[kt][r];
+        }
+        const bf16x8 p = pack8(x[kt], 8 * half);
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(lds.cols_acc(Vl, 32 * kt + 16 * half, ct), p, O[ct]);
+      }
+  };
+  uint16_t *even = smem, *odd = smem + G::BUF;
+  request(0);
+  put(0, even);
+  for (int i = 0; i < nk; i += 2) {             // (two at a time: the buffers' addresses are constants)
+    __syncthreads();
+    if (i + 1 < nk) request(i + 1);
+    tile_of(i, even);
+    if (i + 1 >= nk) break;
+    put(i + 1, odd);
+    __syncthreads();
+    if (i + 2 < nk) request(i + 2);
+    tile_of(i + 1, odd);
+    if (i + 2 < nk) put(i + 2, even);
   }
 
   l = add_xor32(l);
@@ -184,10 +179,9 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a, in
 
 template <int D>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  const int n = a.B * a.H * ((a.L + QT - 1) / QT);
   hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_kernel<D>), Cfg<D>::BYTES);
   if (e != hipSuccess) return e;
-  window_prefill_kernel<D><<<dim3((n + 7) / 8 * 8), 256, Cfg<D>::BYTES, s>>>(a, n);
+  window_prefill_kernel<D><<<dim3((unsigned)xcd_grid(a.B * a.Hkv, a.H / a.Hkv * ((a.L + QT - 1) / QT))), 256, Cfg<D>::BYTES, s>>>(a);
   return hipGetLastError();
 }
 

@@ -26,16 +26,16 @@ struct Cfg {
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a, int n) {
+__global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) float smem_f[];
-  const int place = xcd_place(blockIdx.x, n);
-  if (place >= n) return;
+  const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
+  const int place = xcd_place(blockIdx.x, a.B * a.Hkv, group * ntile);
+  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
+  if (bk >= a.B * a.Hkv) return;
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
-  const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
-  const int g = place % group, tile = place / group % ntile, bk = place / group / ntile;
   const int b = bk / a.Hkv, hk = bk % a.Hkv, h = hk * group + g;
   const int len = clamp_len(a.lens, b, a.L);
   const int t0 = tile * QT, t_end = t0 + QT < a.L ? t0 + QT : a.L;
@@ -157,10 +157,9 @@ __global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a
 
 template <int D>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  const int n = a.B * a.H * ((a.L + QT - 1) / QT);
   hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_f32_kernel<D>), Cfg<D>::FLOATS * 4);
   if (e != hipSuccess) return e;
-  window_prefill_f32_kernel<D><<<dim3((n + 7) / 8 * 8), 256, Cfg<D>::FLOATS * 4, s>>>(a, n);
+  window_prefill_f32_kernel<D><<<dim3((unsigned)xcd_grid(a.B * a.Hkv, a.H / a.Hkv * ((a.L + QT - 1) / QT))), 256, Cfg<D>::FLOATS * 4, s>>>(a);
   return hipGetLastError();
 }
 

@@ -24,31 +24,45 @@ namespace linattn {
 namespace {
 
 constexpr int KT = 32;
+constexpr float kLate = 8.f;                     // log2: how far a running maximum may lie behind before the sums are scaled anew
 constexpr float kNone = -1e30f;                  // the maximum over nothing: finite, so that differences are numbers
 
 template <int D>
 struct MatBf16 {
   typedef uint16_t elem;
   typedef IoBf16 io;
-  static constexpr int RS = D + 16;
-  static constexpr int LDS = KT * RS * 2;        // bytes per wave
+  static constexpr int LDS = KT * D * 2;         // bytes per wave
+  static constexpr int WAVES = 2;                // per SIMD
+  static constexpr int PPR = D / 8;
   bf16x8 q[D / 16], k[D / 16];
   u32x4 v[D / 16];
-  static constexpr int PPR = D / 8;
   __device__ __forceinline__ void load_q(const elem* row, int hi) {
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const bf16x8*>(row + 16 * i + 8 * hi);
   }
-  // key row `key` of this lane; value rows base .. base + 31, those from `rows` on are not there
-  __device__ __forceinline__ void request(const elem* kb, const elem* vb, int key, int base, int rows, int lane) {
-    const elem* kr = kb + (int64_t)key * D + 8 * (lane >> 5);
+  // key row lane % 32 and the value rows of a tile; those from `rows` on are not there (they re-read its row 0)
+  __device__ __forceinline__ void request_k(const elem* kb, int rows, int lane) {
+    const elem* kr = kb + ((lane & 31) < rows ? lane & 31 : 0) * D + 8 * (lane >> 5);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) k[i] = *reinterpret_cast<const bf16x8*>(kr + 16 * i);
+  }
+  __device__ __forceinline__ void request_v(const elem* vb, int rows, int lane) {
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       const int p = lane + 64 * i, r = p / PPR;
-      v[i] = *reinterpret_cast<const u32x4*>(vb + (int64_t)(r < rows ? base + r : 0) * D + p % PPR * 8);
+      v[i] = *reinterpret_cast<const u32x4*>(vb + (r < rows ? r : 0) * D + p % PPR * 8);
     }
+  }
+  // the value rows -> the wave's LDS, from where add() takes them; its registers are free for the next tile's
+  static constexpr bool STAGED = true;
+  __device__ __forceinline__ void stage(unsigned char* lds, int rows, int lane) {
+    uint16_t* Vl = reinterpret_cast<uint16_t*>(lds);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const int e = lane + 64 * i;
+      *reinterpret_cast<u32x4*>(Vl + Swizzled<D>::piece(e / PPR, e % PPR)) = e / PPR < rows ? v[i] : u32x4{0u, 0u, 0u, 0u};
+    }
+    __builtin_amdgcn_wave_barrier();             // (one wave: its LDS operations are served in order)
   }
   __device__ __forceinline__ f32x16 scores() const {
     f32x16 x = {};
@@ -56,19 +70,14 @@ struct MatBf16 {
     for (int i = 0; i < D / 16; ++i) x = mfma(k[i], q[i], x);
     return x;
   }
-  __device__ __forceinline__ void add(f32x16 (&O)[D / 32], const f32x16& p, unsigned char* lds, int rows, int lane) {
-    uint16_t* Vl = reinterpret_cast<uint16_t*>(lds);
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      const int e = lane + 64 * i;
-      *reinterpret_cast<u32x4*>(Vl + e / PPR * RS + e % PPR * 8) = e / PPR < rows ? v[i] : u32x4{0u, 0u, 0u, 0u};
-    }
-    __builtin_amdgcn_wave_barrier();             // (one wave: its LDS operations are served in order)
+  __device__ __forceinline__ void add(f32x16 (&O)[D / 32], const f32x16& p, const unsigned char* lds, int, int lane) {
+    const uint16_t* Vl = reinterpret_cast<const uint16_t*>(lds);
+    const Swizzled<D> at(lane, 4);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const bf16x8 w = pack8(p, 8 * half);
 #pragma unroll
-      for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(tr_operand_acc_order(Vl, RS, 16 * half, 32 * ct, lane), w, O[ct]);
+      for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(at.cols_acc(Vl, 16 * half, ct), w, O[ct]);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -79,23 +88,28 @@ struct MatF32 {
   typedef float elem;
   typedef IoF32 io;
   static constexpr int LDS = 0;
+  static constexpr int WAVES = 1;
+  static constexpr bool STAGED = false;
   f32x4 q[D / 8], k[D / 8];
   float v[16][D / 32];
   __device__ __forceinline__ void load_q(const elem* row, int hi) {
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) q[i] = *reinterpret_cast<const f32x4*>(row + D / 2 * hi + 4 * i);
   }
-  __device__ __forceinline__ void request(const elem* kb, const elem* vb, int key, int base, int rows, int lane) {
-    const elem* kr = kb + (int64_t)key * D + D / 2 * (lane >> 5);
+  __device__ __forceinline__ void request_k(const elem* kb, int rows, int lane) {
+    const elem* kr = kb + ((lane & 31) < rows ? lane & 31 : 0) * D + D / 2 * (lane >> 5);
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) k[i] = *reinterpret_cast<const f32x4*>(kr + 4 * i);
+  }
+  __device__ __forceinline__ void request_v(const elem* vb, int rows, int lane) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int row = acc_row(r, lane >> 5);
 #pragma unroll
-      for (int ct = 0; ct < D / 32; ++ct) v[r][ct] = vb[(int64_t)(row < rows ? base + row : 0) * D + 32 * ct + (lane & 31)];
+      for (int ct = 0; ct < D / 32; ++ct) v[r][ct] = vb[(row < rows ? row : 0) * D + 32 * ct + (lane & 31)];
     }
   }
+  __device__ __forceinline__ void stage(unsigned char*, int, int) {}
   __device__ __forceinline__ f32x16 scores() const {
     f32x16 x = {};
 #pragma unroll
@@ -104,7 +118,7 @@ struct MatF32 {
       for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i][e], q[i][e], x, 0, 0, 0);
     return x;
   }
-  __device__ __forceinline__ void add(f32x16 (&O)[D / 32], const f32x16& p, unsigned char*, int rows, int lane) {
+  __device__ __forceinline__ void add(f32x16 (&O)[D / 32], const f32x16& p, const unsigned char*, int rows, int lane) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const bool in = acc_row(r, lane >> 5) < rows;
@@ -138,11 +152,9 @@ __device__ void commit(const WindowStepArgs& a, int bk, int pos, int n, int tid)
 }
 
 template <template <int> class M, int D>
-__global__ __launch_bounds__(256) void window_step_kernel(WindowStepArgs a) {
+__global__ __launch_bounds__(256, M<D>::WAVES) void window_step_kernel(WindowStepArgs a) {
   typedef typename M<D>::elem E;
-  constexpr int JOIN = 2 * (D / 2 + 2) * 64 * 4;     // two waves' accumulators, maxima, sums
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
-  static_assert(JOIN > 0, "");
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
@@ -150,11 +162,7 @@ __global__ __launch_bounds__(256) void window_step_kernel(WindowStepArgs a) {
   const int b = bk / a.Hkv, hk = bk % a.Hkv, group = a.H / a.Hkv, R = group * a.kk;
   const int r0 = 32 * blockIdx.y, row = r0 + l32;    // this lane's query row: head row / kk of the group, token row % kk
   const int j = row % a.kk;
-  int pos = a.pos[bk];
-  pos = pos < 0 ? 0 : pos;
   const int64_t held = (int64_t)a.sinks + a.window;
-  const int live = pos < held ? pos : (int)held;     // cache rows in use
-  const int nt = (live + KT - 1) / KT + 1;
   const E* kc = static_cast<const E*>(a.kcache) + bk * held * D;
   const E* vc = static_cast<const E*>(a.vcache) + bk * held * D;
   const E* kn = static_cast<const E*>(a.k) + (int64_t)bk * a.kk * D;
@@ -162,20 +170,42 @@ __global__ __launch_bounds__(256) void window_step_kernel(WindowStepArgs a) {
   const int64_t qrow = ((int64_t)b * a.H + hk * group) * a.kk;
   const float c = window_log2_scale(a.scale);
   unsigned char* lds = smem_b + w * M<D>::LDS;
-
   M<D> mat;
+  // Tile i's rows: the step's own, or those of the cache from row (i - 1) KT on.  They are requested before it is known how many
+  // of them are in use (what is not is dropped later): `pos` costs a trip to memory of its own.
+  auto place = [&](int i, const E*& kb, const E*& vb) -> int {
+    if (i == 0) { kb = kn; vb = vn; return a.kk; }
+    const int64_t s0 = (int64_t)(i - 1) * KT;
+    kb = kc + s0 * D; vb = vc + s0 * D;
+    return held - s0 < KT ? (int)(held - s0) : KT;
+  };
+  const int first = split * 4 + w, stride = a.nsplit * 4;
+  const E *kb, *vb;
+  if (first == 0 || (int64_t)(first - 1) * KT < held) {
+    const int n = place(first, kb, vb);
+    mat.request_k(kb, n, lane);
+    mat.request_v(vb, n, lane);
+  }
   mat.load_q(static_cast<const E*>(a.q) + (qrow + (row < R ? row : R - 1)) * D, hi);
+  int pos = a.pos[bk];
+  pos = pos < 0 ? 0 : pos;
+  const int live = pos < held ? pos : (int)held;     // cache rows in use
+  const int nt = (live + KT - 1) / KT + 1;
   f32x16 O[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) O[i] = f32x16{};
   float m = kNone, l = 0.f;
   const int ring = pos - a.sinks;                    // tokens that went into the ring (or less than 0)
-  for (int i = split * 4 + w; i < nt; i += a.nsplit * 4) {
+  for (int i = first; i < nt; i += stride) {
     const int s0 = (i - 1) * KT;                     // the tile's first cache row
     const int rows = i == 0 ? a.kk : live - s0 < KT ? live - s0 : KT;
-    if (i == 0) mat.request(kn, vn, l32 < a.kk ? l32 : 0, 0, rows, lane);
-    else mat.request(kc, vc, l32 < rows ? s0 + l32 : 0, s0, rows, lane);
+    const bool more = i + stride < nt;
+    int n = 0;
+    if (more) n = place(i + stride, kb, vb);
+    mat.stage(lds, rows, lane);
+    if (M<D>::STAGED && more) mat.request_v(vb, n, lane);
     f32x16 x = mat.scores();
+    if (more) mat.request_k(kb, n, lane);
     if (i == 0) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -199,21 +229,21 @@ __global__ __launch_bounds__(256) void window_step_kernel(WindowStepArgs a) {
     float top = x[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
-    const float m2 = fmaxf(m, max_xor32(top) * c);
-    const float f = __builtin_amdgcn_exp2f(m - m2);
-    m = m2;
-    float sum = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r] = __builtin_amdgcn_exp2f(x[r] * c - m2);
-      sum += x[r];
-    }
-    l = l * f + sum;
-    if (__any(f != 1.f)) {
+    top = max_xor32(top) * c;
+    if (__any(top > m + kLate)) {
+      const float m2 = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= f;
 #pragma unroll
       for (int ct = 0; ct < D / 32; ++ct) O[ct] *= f;
     }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(x[r] * c - m);
+      l += x[r];
+    }
     mat.add(O, x, lds, rows, lane);
+    if (!M<D>::STAGED && more) mat.request_v(vb, n, lane);
   }
   l = add_xor32(l);
 
@@ -279,32 +309,54 @@ __global__ __launch_bounds__(256) void window_step_kernel(WindowStepArgs a) {
 template <typename IO, int D>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowStepArgs a) {
   typedef typename IO::elem E;
+  constexpr int LR = D / 4, ROWS = 256 / LR;         // threads of a row, rows of a workgroup
+  __shared__ float weight[ROWS][64];
   const int bk = blockIdx.x, b = bk / a.Hkv, hk = bk % a.Hkv, group = a.H / a.Hkv, R = group * a.kk;
   const int64_t qrow = ((int64_t)b * a.H + hk * group) * a.kk;
-  const int e = blockIdx.y * 256 + threadIdx.x;      // four elements of a row
-  if (a.nsplit > 1 && e < R * (D / 4)) {
-    const int row = e / (D / 4), c = e % (D / 4) * 4;
-    const int64_t at = (int64_t)bk * a.nsplit * R + row;
+  if (a.nsplit > 1) {
+    const int u = threadIdx.x / LR, e = threadIdx.x % LR, row = blockIdx.y * ROWS + u;
+    const int64_t at = (int64_t)bk * a.nsplit * R + (row < R ? row : R - 1);
     const float* stat = a.ws + (int64_t)a.B * a.Hkv * a.nsplit * R * D + 2 * at;
+    // a thread's shares of the row (at most 64, LR of them at a time), the row's maximum and sum over its threads
+    constexpr int EACH = 64 / LR;
+    f32x2 st[EACH];
     float m = kNone;
-    for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, stat[2 * (int64_t)s * R]);
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int s = 0; s < a.nsplit; ++s) {
-      const float lo = stat[2 * (int64_t)s * R + 1];
-      if (lo > 0.f) {
-        const float f = __builtin_amdgcn_exp2f(stat[2 * (int64_t)s * R] - m);
-        l += lo * f;
-        x += f * *reinterpret_cast<const f32x4*>(a.ws + (at + (int64_t)s * R) * D + c);
-      }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int s = e + LR * i;
+      st[i] = s < a.nsplit ? *reinterpret_cast<const f32x2*>(stat + 2 * (int64_t)s * R) : f32x2{kNone, 0.f};
+      m = fmaxf(m, st[i][0]);
     }
-    x *= 1.f / l;
-    E* o = static_cast<E*>(a.out) + (qrow + row) * D + c;
-    if constexpr (sizeof(E) == 2) *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-    else *reinterpret_cast<f32x4*>(o) = x;
+#pragma unroll
+    for (int d = 1; d < LR; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      st[i][0] = st[i][1] > 0.f ? __builtin_amdgcn_exp2f(st[i][0] - m) : 0.f;
+      l += st[i][1] * st[i][0];
+    }
+#pragma unroll
+    for (int d = 1; d < LR; d *= 2) l += __shfl_xor(l, d);
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) weight[u][e + LR * i] = st[i][0] * inv;
+    __syncthreads();
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < a.nsplit; ++s) {
+      const float f = weight[u][s];                  // 0: a share of nothing, which was not written
+      const f32x4 y = *reinterpret_cast<const f32x4*>(a.ws + (at + (int64_t)s * R) * D + 4 * e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] += f > 0.f ? f * y[i] : 0.f;
+    }
+    if (row < R) {
+      E* o = static_cast<E*>(a.out) + (qrow + row) * D + 4 * e;
+      if constexpr (sizeof(E) == 2) *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+      else *reinterpret_cast<f32x4*>(o) = x;
+    }
   }
   if (blockIdx.y == 0) {
-    int pos = a.pos[bk];
+    const int pos = a.pos[bk];
     __syncthreads();
     commit<E, D>(a, bk, pos < 0 ? 0 : pos, kept(a.n_commit, b, a.kk), threadIdx.x);
   }
