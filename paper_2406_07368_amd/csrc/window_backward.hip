@@ -8,8 +8,9 @@
 //   rows of q    128 queries a workgroup, a wave's 32 in its lanes, keys 64 at a time through LDS, as in the prefill:
 //                S^T = K Q^T, dP^T = V dO^T, and dS^T, packed, is the operand of dQ^T += K^T dS^T as it stands.  Writes
 //                delta for the other kernel.
-//   rows of k, v 128 keys of a key/value head a workgroup, a wave's 32 in its lanes, queries 64 at a time through LDS,
-//                over all query heads that share the keys: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+//   rows of k, v 128 keys of a key/value head a workgroup, a wave's 32 in its lanes, queries 32 at a time through LDS,
+//                over all query heads that share the keys: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  The
+//                value rows stay in LDS and not in registers, so that two waves fit a SIMD.
 // Key tile 0 would meet every query of the sequence for the sake of its sinks, many times what other tiles have to do: the
 // query tiles that see nothing of it but sinks are shared out over workgroups of their own, and where there are few key
 // tiles each is shared by several workgroups.  Their sums (fp32) go to the workspace and are added up in a fixed order.
@@ -29,7 +30,8 @@ struct Cfg {
   static constexpr int BUF = 2 * 64 * D;        // elements of one buffer: 64 rows of two tensors
   static constexpr int OS = D + 8;
   static constexpr int TILES = (2 * BUF > 128 * OS ? 2 * BUF : 128 * OS) * 2;   // bytes: the buffers; finished rows
-  static constexpr int BYTES = TILES + 4 * 64 * 4;   // ... and (rows of k, v) lse and delta, two buffers
+  static constexpr int DKV = (128 + 4 * kWindowQ) * D * 2 > 128 * OS * 2 ? (128 + 4 * kWindowQ) * D * 2 : 128 * OS * 2;   // value rows, two buffers; finished rows
+  static constexpr int DKV_BYTES = DKV + 4 * kWindowQ * 4;   // ... and lse and delta, two buffers
   static constexpr int PPR = D / 8;
   static constexpr int CT = D / 32, KS = D / 16;
 };
@@ -111,16 +113,18 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
   const int ns = a.sinks > 0 && lo > 0 ? 1 : 0;
   const int nk = ns + last / 64 - lo + 1;
   auto key0 = [&](int i) { return (i < ns ? i : lo + i - ns) * 64; };
-  Fetch<D> fk, fv;
-  auto request = [&](int i) {
+  const Fetch<D> fetch(tid);
+  auto request = [&](int i, uint16_t* buf) {
     const int s0 = key0(i);
-    fk.request(gk + s0 * a.k.t, a.k.t, len - s0, tid);
-    fv.request(gv + s0 * a.v.t, a.v.t, len - s0, tid);
+    fetch.request(buf, gk + s0 * a.k.t, a.k.t, len - s0);
+    fetch.request(buf + 64 * D, gv + s0 * a.v.t, a.v.t, len - s0);
   };
-  auto put = [&](int i, uint16_t* buf) {
+  auto arrive = [&](int i, uint16_t* buf) {
     const int n = len - key0(i);
-    fk.put(buf, n, tid);
-    fv.put(buf + 64 * D, n, tid);
+    fetch.arrived();
+    fetch.trim(buf, n, tid);
+    fetch.trim(buf + 64 * D, n, tid);
+    __syncthreads();
   };
   f32x16 dQ[G::CT];
 #pragma unroll
@@ -137,6 +141,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
         x = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x);
         y = mfma(lds.rows(Vl, 32 * kt, ks), dop[ks], y);
       }
+      read_ahead<6, 2 * G::KS>();
       const bool all = sw + 31 <= tw && (sw > tw + 31 - a.window || sw + 32 <= a.sinks);
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r] * c - lse2) * (y[r] - delta);
@@ -154,29 +159,27 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
     }
   };
   uint16_t *even = smem, *odd = smem + G::BUF;
-  request(0);
-  put(0, even);
+  request(0, even);
   for (int i = 0; i < nk; i += 2) {
-    __syncthreads();
-    if (i + 1 < nk) request(i + 1);
+    arrive(i, even);
+    if (i + 1 < nk) request(i + 1, odd);
     tile_of(i, even);
     if (i + 1 >= nk) break;
-    put(i + 1, odd);
-    __syncthreads();
-    if (i + 2 < nk) request(i + 2);
+    arrive(i + 1, odd);
+    if (i + 2 < nk) request(i + 2, even);
     tile_of(i + 1, odd);
-    if (i + 2 < nk) put(i + 2, even);
   }
   store_tile<D>(smem, dQ, a.scale, gdq, a.dq.t, t0, t_end, len, tid);
 }
 
 // Jobs of a key/value head: `far` for the sinks (the query tiles from window_far_tile on, with the sinks of key tile 0; the
-// waves take 32 keys and 32 queries of a tile each), then `parts` for every key tile.
+// waves take 32 keys each, and every other of its query tiles), then `parts` for every key tile.
 template <int D>
-__global__ __launch_bounds__(256, 1) void window_dkv_kernel(WindowArgs a) {
+__global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
-  float* stats = reinterpret_cast<float*>(smem + G::TILES / 2);    // [2][lse | delta][64]
+  uint16_t* Vl = smem;                                           // the value rows of the keys
+  float* stats = reinterpret_cast<float*>(smem + G::DKV / 2);    // [2][lse | delta][32]
   const int group = a.H / a.Hkv, each = a.far + a.parts * ((a.L + 127) / 128);
   const int place = xcd_place(blockIdx.x, a.B * a.Hkv, each);
   const int bk = place / each;
@@ -204,105 +207,104 @@ __global__ __launch_bounds__(256, 1) void window_dkv_kernel(WindowArgs a) {
   const Swizzled<D> lds(lane, 4);
   const int kw = sink_job ? 32 * (w & 1) : s0 + 32 * w;          // the wave's first key
   const int s = kw + l32;                                        // this lane's key
-  bf16x8 kop[G::KS], vop[G::KS];
+  bf16x8 kop[G::KS];
   {
     const int row = s < len ? s : 0;
     const uint16_t* pk = static_cast<const uint16_t*>(a.k.p) + b * a.k.b + hk * a.k.h + row * a.k.t + 8 * hi;
-    const uint16_t* pv = static_cast<const uint16_t*>(a.v.p) + b * a.v.b + hk * a.v.h + row * a.v.t + 8 * hi;
 #pragma unroll
-    for (int ks = 0; ks < G::KS; ++ks) {
-      kop[ks] = *reinterpret_cast<const bf16x8*>(pk + 16 * ks);
-      vop[ks] = *reinterpret_cast<const bf16x8*>(pv + 16 * ks);
-    }
+    for (int ks = 0; ks < G::KS; ++ks) kop[ks] = *reinterpret_cast<const bf16x8*>(pk + 16 * ks);
+  }
+  const uint16_t* gv = static_cast<const uint16_t*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const Fetch<D> vfetch(tid);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = s0 + 64 * i, n = len - r > 0 ? len - r : 0;    // (none: row 0 of the sequence, overwritten with zeros)
+    vfetch.request(Vl + i * 64 * D, gv + (n > 0 ? r : 0) * a.v.t, a.v.t, n);
   }
   // query tiles of one head: q_lo .. q_lo + q_n - 1; the items are (head of the group, tile), every step-th of them this workgroup's
-  const int q_len = (len + 63) / 64;
-  const int64_t near_end = ((int64_t)s0 + 127 + a.window - 1) / 64 + 1;   // (key tile 0: window_far_tile)
+  const int q_len = (len + kWindowQ - 1) / kWindowQ;
+  const int64_t near_end = ((int64_t)s0 + 127 + a.window - 1) / kWindowQ + 1;   // (key tile 0: window_far_tile)
   const int end = q_len < near_end ? q_len : (int)near_end;
-  const int q_lo = sink_job ? end : s0 / 64;
+  const int q_lo = sink_job ? end : s0 / kWindowQ;
   const int q_n = (sink_job ? q_len : end) - q_lo > 0 ? (sink_job ? q_len : end) - q_lo : 0;
   const int step = sink_job ? a.far : a.parts;
   const int items = q_n * group;
 
-  Fetch<D> fq, fd;
+  const Fetch<D, kWindowQ> fetch(tid);
   float rs = 0.f;
-  auto first_row = [&](int it) { return (q_lo + it % q_n) * 64; };
-  auto request = [&](int it) {
+  auto first_row = [&](int it) { return (q_lo + it % q_n) * kWindowQ; };
+  auto request = [&](int it, uint16_t* buf) {
     const int h = hk * group + it / q_n, t0 = first_row(it), n = len - t0;
-    fq.request(static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h + t0 * a.q.t, a.q.t, n, tid);
-    fd.request(static_cast<const uint16_t*>(a.dout.p) + b * a.dout.b + h * a.dout.h + t0 * a.dout.t, a.dout.t, n, tid);
-    if (tid < 128) {
-      const int64_t at = ((int64_t)b * a.H + h) * a.L + t0 + (tid & 63);
-      rs = (tid & 63) < n ? (tid < 64 ? a.lse[at] * 1.44269504088896340736f : a.delta[at]) : 0.f;
+    fetch.request(buf, static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h + t0 * a.q.t, a.q.t, n);
+    fetch.request(buf + kWindowQ * D, static_cast<const uint16_t*>(a.dout.p) + b * a.dout.b + h * a.dout.h + t0 * a.dout.t, a.dout.t, n);
+    if (tid < 2 * kWindowQ) {
+      const int64_t at = ((int64_t)b * a.H + h) * a.L + t0 + tid % kWindowQ;
+      rs = tid % kWindowQ < n ? (tid < kWindowQ ? a.lse[at] * 1.44269504088896340736f : a.delta[at]) : 0.f;
     }
   };
-  auto put = [&](int it, uint16_t* buf, float* st) {
+  auto arrive = [&](int it, uint16_t* buf, float* st) {
     const int n = len - first_row(it);
-    fq.put(buf, n, tid);
-    fd.put(buf + 64 * D, n, tid);
-    if (tid < 128) st[tid] = rs;
+    fetch.arrived();
+    fetch.trim(buf, n, tid);
+    fetch.trim(buf + kWindowQ * D, n, tid);
+    if (tid < 2 * kWindowQ) st[tid] = rs;
+    __syncthreads();
   };
 
   f32x16 dK[G::CT], dV[G::CT];
 #pragma unroll
   for (int i = 0; i < G::CT; ++i) { dK[i] = f32x16{}; dV[i] = f32x16{}; }
-  auto tile_of = [&](int it, const uint16_t* Ql, const float* st) {
-    const uint16_t* dl = Ql + 64 * D;
+  auto tile_of = [&](int it, int turn, const uint16_t* Ql, const float* st) {
+    const uint16_t* dl = Ql + kWindowQ * D;
+    const int tw = first_row(it);
+    if (sink_job ? (turn & 1) != w >> 1 || kw >= a.sinks : !(kw <= tw + 31 && (kw + 31 > tw - a.window || kw < a.sinks))) return;
+    f32x16 x = {}, y = {};
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const int tw = first_row(it) + 32 * tt;
-      if (tw >= len) continue;
-      if (sink_job ? tt != w >> 1 || kw >= a.sinks : !(kw <= tw + 31 && (kw + 31 > tw - a.window || kw < a.sinks))) continue;
-      f32x16 x = {}, y = {};
+    for (int ks = 0; ks < G::KS; ++ks) {
+      x = mfma(lds.rows(Ql, 0, ks), kop[ks], x);
+      y = mfma(lds.rows(dl, 0, ks), lds.rows(Vl, kw - s0, ks), y);
+    }
 #pragma unroll
-      for (int ks = 0; ks < G::KS; ++ks) {
-        x = mfma(lds.rows(Ql, 32 * tt, ks), kop[ks], x);
-        y = mfma(lds.rows(dl, 32 * tt, ks), vop[ks], y);
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const f32x4 le = *reinterpret_cast<const f32x4*>(st + 8 * r4 + 4 * hi);
+      const f32x4 de = *reinterpret_cast<const f32x4*>(st + kWindowQ + 8 * r4 + 4 * hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[4 * r4 + i] = __builtin_amdgcn_exp2f(x[4 * r4 + i] * c - le[i]);
+        y[4 * r4 + i] = x[4 * r4 + i] * (y[4 * r4 + i] - de[i]);
       }
+    }
+    const bool all = kw + 31 <= tw && (kw > tw + 31 - a.window || kw + 32 <= a.sinks) && tw + 32 <= len;
+    if (!all) {
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 le = *reinterpret_cast<const f32x4*>(st + 32 * tt + 8 * r4 + 4 * hi);
-        const f32x4 de = *reinterpret_cast<const f32x4*>(st + 64 + 32 * tt + 8 * r4 + 4 * hi);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[4 * r4 + i] = __builtin_amdgcn_exp2f(x[4 * r4 + i] * c - le[i]);
-          y[4 * r4 + i] = x[4 * r4 + i] * (y[4 * r4 + i] - de[i]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int t = tw + acc_row(r, hi);
+        if (!(window_sees(t, s, a.window, a.sinks) && t < len)) { x[r] = 0.f; y[r] = 0.f; }
       }
-      const bool all = kw + 31 <= tw && (kw > tw + 31 - a.window || kw + 32 <= a.sinks) && tw + 32 <= len;
-      if (!all) {
+    }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int t = tw + acc_row(r, hi);
-          if (!(window_sees(t, s, a.window, a.sinks) && t < len)) { x[r] = 0.f; y[r] = 0.f; }
-        }
-      }
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8 p = pack8(x, 8 * half), ds = pack8(y, 8 * half);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const bf16x8 p = pack8(x, 8 * half), ds = pack8(y, 8 * half);
-#pragma unroll
-        for (int ct = 0; ct < G::CT; ++ct) {
-          dV[ct] = mfma(lds.cols_acc(dl, 32 * tt + 16 * half, ct), p, dV[ct]);
-          dK[ct] = mfma(lds.cols_acc(Ql, 32 * tt + 16 * half, ct), ds, dK[ct]);
-        }
+      for (int ct = 0; ct < G::CT; ++ct) {
+        dV[ct] = mfma(lds.cols_acc(dl, 16 * half, ct), p, dV[ct]);
+        dK[ct] = mfma(lds.cols_acc(Ql, 16 * half, ct), ds, dK[ct]);
       }
     }
   };
-  uint16_t *even = smem, *odd = smem + G::BUF;
-  if (part < items) {
-    request(part);
-    put(part, even, stats);
-  }
-  for (int it = part; it < items; it += 2 * step) {
-    __syncthreads();
-    if (it + step < items) request(it + step);
-    tile_of(it, even, stats);
+  uint16_t *even = smem + 128 * D, *odd = even + 2 * kWindowQ * D;
+  if (part < items) request(part, even);
+  vfetch.arrived();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) vfetch.trim(Vl + i * 64 * D, len - s0 - 64 * i, tid);
+  for (int it = part, turn = 0; it < items; it += 2 * step, turn += 2) {
+    arrive(it, even, stats);
+    if (it + step < items) request(it + step, odd);
+    tile_of(it, turn, even, stats);
     if (it + step >= items) break;
-    put(it + step, odd, stats + 128);
-    __syncthreads();
-    if (it + 2 * step < items) request(it + 2 * step);
-    tile_of(it + step, odd, stats + 128);
-    if (it + 2 * step < items) put(it + 2 * step, even, stats);
+    arrive(it + step, odd, stats + 2 * kWindowQ);
+    if (it + 2 * step < items) request(it + 2 * step, even);
+    tile_of(it + step, turn + 1, odd, stats + 2 * kWindowQ);
   }
   if (!sink_job && a.parts == 1) {
     store_tile<D>(smem, dK, a.scale, gdk, a.dk.t, s0, s_end, len, tid);
@@ -361,13 +363,13 @@ __global__ __launch_bounds__(256) void window_shares_kernel(WindowArgs a) {
 template <int D>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   const int heads = a.B * a.Hkv, tiles = (a.L + 127) / 128;
-  hipError_t e = LINATTN_MAX_LDS_ONCE((window_dq_kernel<D>), Cfg<D>::BYTES);
+  hipError_t e = LINATTN_MAX_LDS_ONCE((window_dq_kernel<D>), Cfg<D>::TILES);
   if (e != hipSuccess) return e;
-  e = LINATTN_MAX_LDS_ONCE((window_dkv_kernel<D>), Cfg<D>::BYTES);
+  e = LINATTN_MAX_LDS_ONCE((window_dkv_kernel<D>), Cfg<D>::DKV_BYTES);
   if (e != hipSuccess) return e;
-  window_dq_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.H / a.Hkv * tiles)), 256, Cfg<D>::BYTES, s>>>(a);
+  window_dq_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.H / a.Hkv * tiles)), 256, Cfg<D>::TILES, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  window_dkv_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.far + a.parts * tiles)), 256, Cfg<D>::BYTES, s>>>(a);
+  window_dkv_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.far + a.parts * tiles)), 256, Cfg<D>::DKV_BYTES, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.parts > 1) {
     constexpr int PER = 1024 / D;

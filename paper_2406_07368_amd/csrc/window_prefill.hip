@@ -78,16 +78,18 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
   const int nk = ns + last / KT - lo + 1;
   auto key0 = [&](int i) { return (i < ns ? i : lo + i - ns) * KT; };
 
-  Fetch<D> fk, fv;
-  auto request = [&](int i) {
+  const Fetch<D> fetch(tid);
+  auto request = [&](int i, uint16_t* buf) {
     const int s0 = key0(i);
-    fk.request(gk + s0 * a.k.t, a.k.t, len - s0, tid);
-    fv.request(gv + s0 * a.v.t, a.v.t, len - s0, tid);
+    fetch.request(buf, gk + s0 * a.k.t, a.k.t, len - s0);
+    fetch.request(buf + KT * D, gv + s0 * a.v.t, a.v.t, len - s0);
   };
-  auto put = [&](int i, uint16_t* buf) {
+  auto arrive = [&](int i, uint16_t* buf) {     // ... and, behind the barrier, everybody's
     const int n = len - key0(i);
-    fk.put(buf, n, tid);
-    fv.put(buf + KT * D, n, tid);
+    fetch.arrived();
+    fetch.trim(buf, n, tid);
+    fetch.trim(buf + KT * D, n, tid);
+    __syncthreads();
   };
 
   f32x16 O[D / 32];
@@ -104,6 +106,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) x[kt] = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x[kt]);
+    read_ahead<6, D / 8>();
     const bool all = s0 + KT - 1 <= tw && (s0 > tw + 31 - a.window || s0 + KT <= a.sinks);
     if (!all) {
 #pragma unroll
@@ -142,18 +145,15 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
       }
   };
   uint16_t *even = smem, *odd = smem + G::BUF;
-  request(0);
-  put(0, even);
+  request(0, even);
   for (int i = 0; i < nk; i += 2) {             // (two at a time: the buffers' addresses are constants)
-    __syncthreads();
-    if (i + 1 < nk) request(i + 1);
+    arrive(i, even);
+    if (i + 1 < nk) request(i + 1, odd);
     tile_of(i, even);
     if (i + 1 >= nk) break;
-    put(i + 1, odd);
-    __syncthreads();
-    if (i + 2 < nk) request(i + 2);
+    arrive(i + 1, odd);
+    if (i + 2 < nk) request(i + 2, even);
     tile_of(i + 1, odd);
-    if (i + 2 < nk) put(i + 2, even);
   }
 
   l = add_xor32(l);
