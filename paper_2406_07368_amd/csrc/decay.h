@@ -28,6 +28,7 @@ struct DecayArgs {
   float* ws;               // nseg > 1: [B*H][roles][nseg][d*d], the state before every segment
   int B, H, L;
   int nseg, seg_len;       // segments of seg_len tokens (a multiple of 64), in the order of the walk
+  int fold;                // few segments: the workspace holds what each adds, and each sums up those before it
   float scale;
   int exact_state;         // what enters the state carries sixteen significant bits (else eight: the gradient's own states)
 };

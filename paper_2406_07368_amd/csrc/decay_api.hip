@@ -39,6 +39,10 @@ __global__ __launch_bounds__(256) void state_through_kernel(const float* from, f
   for (int i = threadIdx.x; i < dd; i += 256) to[(size_t)blockIdx.x * dd + i] = from ? from[(size_t)blockIdx.x * dd + i] : 0.f;
 }
 
+// Up to so many segments every segment sums up for itself what those before it add (64 KB each at d = 128, from the L2 cache)
+// instead of a launch that does.
+constexpr int kFold = 8;
+
 struct Plan {
   int nseg, seg_len;
   size_t bytes;
@@ -83,7 +87,8 @@ linattn_status run(DecayArgs& a, const linattn_decay_desc* d, const Plan& p, voi
   hipError_t e = hipSuccess;
   if (p.nseg > 1) {
     e = bf16 ? launch_decay_first_pass_bf16(a, d->d, s) : launch_decay_first_pass_f32(a, d->d, s);
-    if (e == hipSuccess) {
+    a.fold = p.nseg <= kFold;
+    if (e == hipSuccess && !a.fold) {
       const int dd = d->d * d->d;
       decay_scan_kernel<<<dim3(a.roles * a.B * a.H * (dd / 256)), 256, 0, s>>>(a, dd);
       e = hipGetLastError();

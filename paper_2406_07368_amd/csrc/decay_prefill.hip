@@ -8,10 +8,12 @@
 //   S   <- lambda^n S + K^T V',                  v'_j = lambda^{n-1-j} v_j
 //
 // Every power has an exponent >= 0, so nothing overflows however fast a head forgets.  One workgroup walks one head (or
-// a segment of it); wave w owns the value columns 32w .. 32w+31: S[:, 32w..] stays in its accumulators, and is its own
-// MFMA operand for the read-out (the accumulator layout is the operand layout up to a permutation of the contraction
-// index, which is applied to Q's LDS address).  The rows are requested one group ahead into registers and go to one of
-// two LDS buffers; the finished rows go back through the Q rows of their own buffer, so that whole rows are stored.
+// a segment of it), two waves on every SIMD.  Wave (ct, half) owns the value columns 32ct .. 32ct+31 and one half of S's rows
+// for the state, and one half of the group's tokens for the outputs: S[half, 32ct..] stays in its accumulators and, packed, is
+// the MFMA operand of the read-out as it stands (the rows' order in the accumulators is made so by the order in which K is
+// read); it reads for all 64 tokens and gives the other wave of the pair, through LDS, what that one's tokens get from its
+// rows.  The scores are ten 16 x 16 tiles, dealt out over the waves.  Rows come straight into one of two LDS buffers while
+// the other is worked on (swizzle.h); finished rows leave through LDS, so that whole rows are stored.
 // V' enters the state as the sum of two bf16 terms (sixteen significant bits: S is handed back in fp32 and lives on in
 // generation); where the state is only this launch's own (the gradient) one term is enough.
 //
@@ -22,7 +24,7 @@
 #include "common.h"
 #include "decay.h"
 #include "kernels.h"
-#include "mfma_util.h"
+#include "swizzle.h"
 
 namespace linattn {
 
@@ -32,18 +34,19 @@ constexpr int C = 64;                       // tokens per group
 
 template <int D>
 struct Cfg {
-  static constexpr int NW = D / 32, NT = 64 * NW;
-  static constexpr int RS = D + 16;         // LDS row stride
-  static constexpr int PS = C + 8;
-  static constexpr int BUF = 3 * C * RS;    // elements of one buffer: Q, K, V
-  static constexpr int BYTES = (2 * BUF + C * PS) * 2;
-  static constexpr int PPR = D / 8;         // 16-byte pieces per row
-  static constexpr int NP = C * PPR / NT;   // pieces per thread and tensor
-  static constexpr int RT = D / 32;         // 32-row tiles of S
-  static constexpr int TW = (3 + NW - 1) / NW;   // score tiles per wave
+  static constexpr int NW = D / 16, NT = 64 * NW;
+  static constexpr int CT = D / 32;              // column tiles of S: the waves 0 .. CT-1 have its upper rows, the others its lower
+  static constexpr int IT = D / 64;              // 32-row tiles of a wave's S
+  static constexpr int TILE = C * D;             // elements of one tensor's rows
+  static constexpr int PPR = D / 8;
+  static constexpr int NP = C * PPR / NT;        // 16-byte pieces of a tensor's rows per thread
+  static constexpr int TW = (10 + NW - 1) / NW;  // score tiles per wave
+  // bytes: two buffers of K, V (, Q); P; what the waves of a pair give each other; finished rows
+  static constexpr int KV = 4 * TILE * 2;
+  static constexpr int OFF_P = 6 * TILE * 2, OFF_X = OFF_P + C * C * 2, OFF_O = OFF_X + NW * 1024 * 4, ALL = OFF_O + TILE * 2;
 };
 
-struct Walk {                               // where one tensor's rows of this (b, h) are
+struct Walk {                                    // one tensor's rows of this (b, h)
   const uint16_t* p;
   int64_t t;
 };
@@ -52,13 +55,15 @@ __device__ __forceinline__ Walk walk(const Rows& r, int b, int h) {
 }
 
 template <int D, bool STATE_ONLY, bool TWO>
-__global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_kernel(DecayArgs a) {
+__global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
-  uint16_t* Pl = smem + 2 * G::BUF;
+  uint16_t* Pl = smem + G::OFF_P / 2;
+  float* Xl = reinterpret_cast<float*>(smem + G::OFF_X / 2);
+  uint16_t* Ol = smem + G::OFF_O / 2;
   const int tid = threadIdx.x;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), ct = w % G::CT, half = w / G::CT;
+  const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5, l16 = lane & 15, q4 = lane >> 4;
   const int seg = blockIdx.x % a.nseg, bhr = blockIdx.x / a.nseg;
   const int bh = bhr / a.roles, b = bh / a.H, h = bh % a.H;   // (the roles of a head side by side: they read the same rows)
   const DecayRole& role = a.role[bhr % a.roles];
@@ -70,130 +75,145 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_kernel(DecayArgs 
   const float g2 = decay_log2(a.log_decay, h);
   float* slot = a.ws + ((size_t)bhr * a.nseg + seg) * (D * D);
   if (STATE_ONLY && seg == a.nseg - 1) return;   // nothing starts behind the last segment
-  const int c0 = 32 * w;
 
-  // ---- the state's 32 columns: row (r&3) + 8(r>>2) + 4hi of tile it, column c0 + l32
-  f32x16 S[G::RT];
-  const float* S0 = STATE_ONLY ? nullptr : a.nseg > 1 ? slot : a.S_in ? a.S_in + (size_t)bh * D * D : nullptr;
-#pragma unroll
-  for (int it = 0; it < G::RT; ++it)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) S[it][r] = S0 ? S0[(32 * it + (r & 3) + 8 * (r >> 2) + 4 * hi) * D + c0 + l32] : 0.f;
+  const int live_end = t_end < len ? t_end : len;                        // tokens that are there
+  const int ng = live_end > t_begin ? (live_end - t_begin + C - 1) / C : 0;
+  const Fetch<D, C, G::NT> fetch(tid);
+  auto buffer = [&](int i) { return smem + i * (STATE_ONLY ? 2 : 3) * G::TILE; };   // K, V, Q
+  auto request = [&](int gi) {
+    const int tok0 = t_begin + gi * C, n = live_end - tok0;
+    uint16_t* buf = buffer(gi & 1);
+    auto one = [&](uint16_t* to, const Walk& from) {
+      if (reverse) fetch.template request<true>(to, from.p + (int64_t)(len - tok0 - (n < C ? n : C)) * from.t, from.t, n);
+      else fetch.request(to, from.p + (int64_t)tok0 * from.t, from.t, n);
+    };
+    one(buf, wk);
+    one(buf + G::TILE, wv);
+    if (!STATE_ONLY) one(buf + 2 * G::TILE, wq);
+  };
+  auto arrive = [&](int gi) {
+    const int n = live_end - (t_begin + gi * C);
+    uint16_t* buf = buffer(gi & 1);
+    fetch.arrived();
+    fetch.trim(buf, n, tid);
+    fetch.trim(buf + G::TILE, n, tid);
+    if (!STATE_ONLY) fetch.trim(buf + 2 * G::TILE, n, tid);
+    __syncthreads();
+  };
+  if (ng > 0) request(0);
 
-  // ---- powers of the decay that every whole group uses
-  f32x16 fac[G::TW];                        // this wave's score tiles: number w, w + NW, .. of (0,0), (1,0), (1,1)
+  // ---- this wave's part of the state: register r of tile it is row 32 (G::IT half + it) + row_of(r), column 32 ct + l32
+  auto row_of = [&](int r) { return 16 * (r >> 3) + 8 * hi + (r & 7); };
+  auto at = [&](int it, int r) { return (32 * (G::IT * half + it) + row_of(r)) * D + 32 * ct + l32; };
+  f32x16 S[G::IT];
+  const float* S0 = STATE_ONLY ? nullptr : a.nseg > 1 && !a.fold ? slot : a.S_in ? a.S_in + (size_t)bh * D * D : nullptr;
 #pragma unroll
-  for (int i = 0; i < G::TW; ++i) {
-    const int n = w + i * G::NW, tt = n > 0, st = n > 1;
+  for (int it = 0; it < G::IT; ++it)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int gap = 32 * (tt - st) + l32 - ((r & 3) + 8 * (r >> 2) + 4 * hi);
-      fac[i][r] = gap >= 0 ? decay_pow(g2, gap) : 0.f;
+    for (int r = 0; r < 16; ++r) S[it][r] = S0 ? S0[at(it, r)] : 0.f;
+  if (!STATE_ONLY && a.nseg > 1 && a.fold) {     // few segments: what those before this one add, instead of a launch that sums it up
+    for (int j = 0; j < seg; ++j) {
+      const float* inc = a.ws + ((size_t)bhr * a.nseg + j) * (D * D);
+      const int left = len - j * a.seg_len, n = left < 0 ? 0 : left > a.seg_len ? a.seg_len : left;
+      const float keep = decay_pow(g2, n);
+#pragma unroll
+      for (int it = 0; it < G::IT; ++it)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[it][r] = S[it][r] * keep + inc[at(it, r)];
     }
   }
-  const float fq0 = decay_pow(g2, l32 + 1) * a.scale, fq1 = decay_pow(g2, l32 + 33) * a.scale;
-  float fv[4][8];                           // of the rows 16ks + 8hi + j of a group
+
+  // ---- powers of the decay that every whole group uses
+  // score tile n of 10: (tb, sb) with sb <= tb; a lane has query 16 tb + l16 and keys 16 sb + 4 q4 + 0..3
+  auto tile_row = [](int n) { return n >= 6 ? 3 : n >= 3 ? 2 : n >= 1 ? 1 : 0; };
+  f32x4 fac[G::TW];
+#pragma unroll
+  for (int i = 0; i < G::TW; ++i) {
+    const int n = w + i * G::NW, tb = tile_row(n), sb = n - tb * (tb + 1) / 2;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int gap = 16 * (tb - sb) + l16 - (4 * q4 + r);
+      fac[i][r] = gap >= 0 ? decay_pow(g2, gap) * a.scale : 0.f;
+    }
+  }
+  const float fq = decay_pow(g2, 32 * half + l32 + 1) * a.scale;         // of this wave's queries
+  float fv[4][8];                                                        // of the rows 16ks + 8hi + j of a group
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
     for (int j = 0; j < 8; ++j) fv[ks][j] = decay_pow(g2, 63 - (16 * ks + 8 * hi + j));
 
-  u32x4 rq[G::NP], rk[G::NP], rv[G::NP];
-  auto request = [&](int tok0) {            // rows past the end re-read row 0; they are dropped in put()
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + G::NT * i, t = tok0 + p / G::PPR, c = p % G::PPR * 8;
-      const int row = t < t_end && t < len ? walk_row(t, len, reverse) : 0;
-      if (!STATE_ONLY) rq[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wq.p + row * wq.t + c));
-      rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wk.p + row * wk.t + c));
-      rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wv.p + row * wv.t + c));
-    }
-  };
-  auto put = [&](int tok0, uint16_t* buf) {
-#pragma unroll
-    for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + G::NT * i, t = tok0 + p / G::PPR;
-      uint16_t* d = buf + p / G::PPR * G::RS + p % G::PPR * 8;
-      const bool in = t < t_end && t < len;
-      const u32x4 z = {0u, 0u, 0u, 0u};
-      if (!STATE_ONLY) *reinterpret_cast<u32x4*>(d) = in ? rq[i] : z;
-      *reinterpret_cast<u32x4*>(d + C * G::RS) = in ? rk[i] : z;
-      *reinterpret_cast<u32x4*>(d + 2 * C * G::RS) = in ? rv[i] : z;
-    }
-  };
   uint16_t* gout = const_cast<uint16_t*>(wo.p);
-  auto store_rows = [&](int tok0, const uint16_t* buf) {
+  auto store_rows = [&](int gi) {
+    const int tok0 = t_begin + gi * C;
 #pragma unroll
     for (int i = 0; i < G::NP; ++i) {
       const int p = tid + G::NT * i, t = tok0 + p / G::PPR;
       if (t < t_end) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(buf + p / G::PPR * G::RS + p % G::PPR * 8), z = {0u, 0u, 0u, 0u};
+        const u32x4 x = *reinterpret_cast<const u32x4*>(Ol + Swizzled<D>::piece(p / G::PPR, p % G::PPR)), z = {0u, 0u, 0u, 0u};
         __builtin_nontemporal_store(t < len ? x : z, reinterpret_cast<u32x4*>(gout + walk_row(t, len, reverse) * wo.t + p % G::PPR * 8));
       }
     }
   };
+  // the tiles of P that are read but hold only later keys, (0, 1) and (2, 3), stay zeros
+  if (!STATE_ONLY)
+    for (int i = tid; i < C * C / 8; i += G::NT) *reinterpret_cast<u32x4*>(Pl + 8 * i) = u32x4{0u, 0u, 0u, 0u};
+  const Swizzled<D> kv(lane, 8), kx(lane, 8, true);
+  const Swizzled<C> pr(lane, 8);
 
-  const int live_end = t_end < len ? t_end : len;                       // tokens that are there
-  const int ng = live_end > t_begin ? (live_end - t_begin + C - 1) / C : 0;
-  if (ng > 0) {
-    request(t_begin);
-    put(t_begin, smem);
-  }
   for (int gi = 0; gi < ng; ++gi) {
     const int tok0 = t_begin + gi * C;
-    uint16_t* buf = smem + (gi & 1) * G::BUF;
-    uint16_t *Ql = buf, *Kl = buf + C * G::RS, *Vl = buf + 2 * C * G::RS;
+    const uint16_t *Kl = buffer(gi & 1), *Vl = Kl + G::TILE, *Ql = Vl + G::TILE;
     const int n = live_end - tok0 < C ? live_end - tok0 : C;
-    __syncthreads();                        // the group's rows, and the finished rows of the group before
-    if (gi + 1 < ng) request(tok0 + C);
-    if (!STATE_ONLY && gi > 0) store_rows(tok0 - C, smem + ((gi + 1) & 1) * G::BUF);
+    arrive(gi);                                  // the group's rows; the finished rows of the group before
+    if (gi + 1 < ng) request(gi + 1);
+    if (!STATE_ONLY && gi > 0) store_rows(gi - 1);
 
-    bf16x8 vop[4];                          // V[16ks + 8hi + 0..7][c0 + l32]
+    bf16x8 vop[4];                               // V[16ks + 8hi + 0..7][32 ct + l32]
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) vop[ks] = tr_operand(Vl, G::RS, 16 * ks, c0, lane);
+    for (int ks = 0; ks < 4; ++ks) vop[ks] = kv.cols(Vl, 16 * ks, ct);
 
     f32x16 O[2];
     if (!STATE_ONLY) {
       // ---- this wave's tiles of P^T, weighted
 #pragma unroll
       for (int i = 0; i < G::TW; ++i) {
-        const int nt = w + i * G::NW, tt = nt > 0, st = nt > 1;
-        if (nt < 3) {
-          f32x16 x = {};
+        const int nt = w + i * G::NW, tb = tile_row(nt), sb = nt - tb * (tb + 1) / 2;
+        if (nt < 10) {
+          f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            x = mfma(lds_row8(Kl + (32 * st + l32) * G::RS + 16 * ks + 8 * hi), lds_row8(Ql + (32 * tt + l32) * G::RS + 16 * ks + 8 * hi), x);
+          for (int ks = 0; ks < D / 32; ++ks)
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row8(Kl + Swizzled<D>::piece(16 * sb + l16, 4 * ks + q4)),
+                                                        lds_row8(Ql + Swizzled<D>::piece(16 * tb + l16, 4 * ks + q4)), x, 0, 0, 0);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = fac[i][r] != 0.f ? x[r] * fac[i][r] * a.scale : 0.f;
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            const u32x2 y = {pack_bf16x2(x[4 * r4], x[4 * r4 + 1]), pack_bf16x2(x[4 * r4 + 2], x[4 * r4 + 3])};
-            *reinterpret_cast<u32x2*>(Pl + (32 * tt + l32) * G::PS + 32 * st + 8 * r4 + 4 * hi) = y;
-          }
+          for (int r = 0; r < 4; ++r) x[r] = fac[i][r] != 0.f ? x[r] * fac[i][r] : 0.f;
+          *reinterpret_cast<u32x2*>(Pl + Swizzled<C>::piece(16 * tb + l16, 2 * sb + (q4 >> 1)) + 4 * (q4 & 1)) =
+              u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
         }
       }
-      // ---- S^T Q^T
+      // ---- S^T Q^T over this wave's rows of S, all queries
       O[0] = f32x16{}; O[1] = f32x16{};
 #pragma unroll
-      for (int it = 0; it < G::RT; ++it)
+      for (int it = 0; it < G::IT; ++it)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const bf16x8 s = pack8(S[it], 8 * half);
+        for (int ks = 0; ks < 2; ++ks) {
+          const bf16x8 s = pack8(S[it], 8 * ks);
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            const uint16_t* q = Ql + (32 * tt + l32) * G::RS + 32 * it + 16 * half + 4 * hi;
-            O[tt] = mfma(s, cat4(lds_row4(q), lds_row4(q + 8)), O[tt]);
-          }
+          for (int tt = 0; tt < 2; ++tt) O[tt] = mfma(s, kv.rows(Ql, 32 * tt, 2 * (G::IT * half + it) + ks), O[tt]);
         }
-      O[0] *= fq0; O[1] *= fq1;
+      const f32x16 away = half ? O[0] : O[1];    // the other wave's queries
+      if (half) O[0] = O[1];
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(Xl + (w * 4 + r4) * 256 + 4 * lane) = f32x4{away[4 * r4], away[4 * r4 + 1], away[4 * r4 + 2], away[4 * r4 + 3]};
     }
     // ---- the state takes the group
     const float keep = decay_pow(g2, n);
 #pragma unroll
-    for (int it = 0; it < G::RT; ++it) S[it] *= keep;
+    for (int it = 0; it < G::IT; ++it) S[it] *= keep;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      f32x16 x;                             // eight values; split8 and pack8 take them from an accumulator
+      f32x16 x;                                  // eight values; split8 and pack8 take them from an accumulator
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int i = 16 * ks + 8 * hi + j;
@@ -204,32 +224,34 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_kernel(DecayArgs 
       if (TWO) split8(x, 0, vh, vo);
       else vh = pack8(x, 0);
 #pragma unroll
-      for (int it = 0; it < G::RT; ++it) {
-        const bf16x8 k = tr_operand(Kl, G::RS, 16 * ks, 32 * it, lane);
+      for (int it = 0; it < G::IT; ++it) {
+        const bf16x8 k = kx.cols(Kl, 16 * ks, G::IT * half + it);
         S[it] = mfma(k, vh, S[it]);
         if (TWO) S[it] = mfma(k, vo, S[it]);
       }
     }
     if (!STATE_ONLY) {
-      __syncthreads();                      // P; and every wave is done with the Q rows
+      __syncthreads();                           // P; the read-outs from the other half's rows
+      const float* X = Xl + ((w + G::CT) % G::NW * 4) * 256 + 4 * lane;
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(X + r4 * 256);
 #pragma unroll
-        for (int ks = 0; ks < 2 * (tt + 1); ++ks)
-          O[tt] = mfma(vop[ks], lds_row8(Pl + (32 * tt + l32) * G::PS + 16 * ks + 8 * hi), O[tt]);
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const u32x2 y = {pack_bf16x2(O[tt][4 * r4], O[tt][4 * r4 + 1]), pack_bf16x2(O[tt][4 * r4 + 2], O[tt][4 * r4 + 3])};
-          *reinterpret_cast<u32x2*>(Ql + (32 * tt + l32) * G::RS + c0 + 8 * r4 + 4 * hi) = y;
-        }
+        for (int i = 0; i < 4; ++i) O[0][4 * r4 + i] = (O[0][4 * r4 + i] + y[i]) * fq;
       }
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+        if (ks < 2 || half) O[0] = mfma(vop[ks], pr.rows(Pl, 32 * half, ks), O[0]);
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<u32x2*>(Ol + Swizzled<D>::piece(32 * half + l32, 4 * ct + r4) + 4 * hi) =
+            u32x2{pack_bf16x2(O[0][4 * r4], O[0][4 * r4 + 1]), pack_bf16x2(O[0][4 * r4 + 2], O[0][4 * r4 + 3])};
     }
-    if (gi + 1 < ng) put(tok0 + C, smem + ((gi + 1) & 1) * G::BUF);
   }
   if (!STATE_ONLY) {
     if (ng > 0) {
       __syncthreads();
-      store_rows(t_begin + (ng - 1) * C, smem + ((ng - 1) & 1) * G::BUF);
+      store_rows(ng - 1);
     }
     // rows behind the end of the sequence, in groups that the walk has not met
     for (int e = tid; e < (t_end - t_begin - ng * C) * G::PPR; e += G::NT) {
@@ -240,18 +262,19 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_kernel(DecayArgs 
   float* So = STATE_ONLY ? slot : a.S_out && seg == a.nseg - 1 ? a.S_out + (size_t)bh * D * D : nullptr;
   if (So) {
 #pragma unroll
-    for (int it = 0; it < G::RT; ++it)
+    for (int it = 0; it < G::IT; ++it)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) So[(32 * it + (r & 3) + 8 * (r >> 2) + 4 * hi) * D + c0 + l32] = S[it][r];
+      for (int r = 0; r < 16; ++r) So[at(it, r)] = S[it][r];
   }
 }
 
 template <int D, bool STATE_ONLY, bool TWO>
 hipError_t launch(const DecayArgs& a, hipStream_t s) {
   using G = Cfg<D>;
-  hipError_t e = LINATTN_MAX_LDS_ONCE((decay_prefill_kernel<D, STATE_ONLY, TWO>), G::BYTES);
+  constexpr int bytes = STATE_ONLY ? G::KV : G::ALL;
+  hipError_t e = LINATTN_MAX_LDS_ONCE((decay_prefill_kernel<D, STATE_ONLY, TWO>), bytes);
   if (e != hipSuccess) return e;
-  decay_prefill_kernel<D, STATE_ONLY, TWO><<<dim3(a.roles * a.B * a.H * a.nseg), G::NT, G::BYTES, s>>>(a);
+  decay_prefill_kernel<D, STATE_ONLY, TWO><<<dim3(a.roles * a.B * a.H * a.nseg), G::NT, bytes, s>>>(a);
   return hipGetLastError();
 }
 

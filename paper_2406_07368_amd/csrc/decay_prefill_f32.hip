@@ -58,11 +58,23 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
   const int c0 = 32 * w;
 
   f32x16 S[G::RT];
-  const float* S0 = STATE_ONLY ? nullptr : a.nseg > 1 ? slot : a.S_in ? a.S_in + (size_t)bh * D * D : nullptr;
+  const float* S0 = STATE_ONLY ? nullptr : a.nseg > 1 && !a.fold ? slot : a.S_in ? a.S_in + (size_t)bh * D * D : nullptr;
 #pragma unroll
   for (int it = 0; it < G::RT; ++it)
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[it][r] = S0 ? S0[(32 * it + acc_row(r, hi)) * D + c0 + l32] : 0.f;
+
+  if (!STATE_ONLY && a.nseg > 1 && a.fold) {
+    for (int j = 0; j < seg; ++j) {
+      const float* inc = a.ws + ((size_t)bhr * a.nseg + j) * (D * D);
+      const int left = len - j * a.seg_len, n = left < 0 ? 0 : left > a.seg_len ? a.seg_len : left;
+      const float keep = decay_pow(g2, n);
+#pragma unroll
+      for (int it = 0; it < G::RT; ++it)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[it][r] = S[it][r] * keep + inc[(32 * it + acc_row(r, hi)) * D + c0 + l32];
+    }
+  }
 
   float fp[16], fv[16];                     // of the scores (key acc_row(r), query l32); of the value rows acc_row(r)
 #pragma unroll

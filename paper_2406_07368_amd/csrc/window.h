@@ -88,51 +88,4 @@ __device__ __forceinline__ int xcd_place(int block, int units, int each) {
   return u < units ? u * each + i % each : units * each;
 }
 
-// For a run of N products whose operands (one LDS read each) the compiler would fetch one by one, each product waiting for its
-// own: the first A reads, then product and read in turn.
-template <int A, int N>
-__device__ __forceinline__ void read_ahead() {
-  __builtin_amdgcn_sched_group_barrier(0x100, A, 0);      // LDS reads
-#pragma unroll
-  for (int i = 0; i < N - A; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // MFMA
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-  }
-  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
-}
-
-// ROWS rows of D bf16 from memory straight into LDS (swizzle.h), 256 threads: a wave's request fills 1 KB in the order of its
-// lanes, so a lane asks for the piece that belongs at its place.  `rows` of them are there: the others re-read row 0 and are
-// overwritten with zeros (by the thread that asked for them) once they are in.
-template <int D, int ROWS = 64>
-struct Fetch {
-  static constexpr int PPR = D / 8, NP = ROWS * PPR / 256, RP = 256 / PPR;   // (RP rows on: the same permutation)
-  typedef const __attribute__((address_space(1))) void* global_ptr;
-  typedef __attribute__((address_space(3))) void* lds_ptr;
-  uint32_t row, piece;
-  int wave;
-  __device__ __forceinline__ explicit Fetch(int tid)
-      : row(tid / PPR), piece(((tid % PPR) ^ Swizzled<D>::f(tid / PPR)) * 8), wave(__builtin_amdgcn_readfirstlane(tid >> 6)) {}
-  __device__ __forceinline__ void request(uint16_t* lds, const uint16_t* row0, int64_t stride, int rows) const {
-    const uint32_t st = (uint32_t)stride;                 // (at most 2^22: a tile's offsets fit 32 bits)
-    const char* base = reinterpret_cast<const char*>(row0);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      uint32_t r = row + RP * i;
-      if (rows < ROWS) r = r < (uint32_t)rows ? r : 0;
-      __builtin_amdgcn_global_load_lds((global_ptr)(base + (r * st + piece) * 2), (lds_ptr)(lds + (i * 256 + wave * 64) * 8), 16, 0, 0);
-    }
-  }
-  // behind arrived()
-  __device__ __forceinline__ void trim(uint16_t* lds, int rows, int tid) const {
-    if (rows < ROWS) {
-#pragma unroll
-      for (int i = 0; i < NP; ++i)
-        if ((int)row + RP * i >= rows) *reinterpret_cast<u32x4*>(lds + (i * 256 + tid) * 8) = u32x4{0u, 0u, 0u, 0u};
-    }
-  }
-  // this wave's requests are in LDS (a barrier makes them everybody's)
-  static __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }
-};
-
 }  // namespace linattn
