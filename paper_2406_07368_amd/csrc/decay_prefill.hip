@@ -143,6 +143,7 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
 #pragma unroll
     for (int j = 0; j < 8; ++j) fv[ks][j] = decay_pow(g2, 63 - (16 * ks + 8 * hi + j));
 
+  const float keep64 = decay_pow(g2, C);
   uint16_t* gout = const_cast<uint16_t*>(wo.p);
   auto store_rows = [&](int gi) {
     const int tok0 = t_begin + gi * C;
@@ -169,11 +170,20 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
     if (gi + 1 < ng) request(gi + 1);
     if (!STATE_ONLY && gi > 0) store_rows(gi - 1);
 
+    if (n < C) {                                 // (the last group of all: the powers are not needed again)
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int i = 16 * ks + 8 * hi + j;
+          fv[ks][j] = i < n ? decay_pow(g2, n - 1 - i) : 0.f;
+        }
+    }
     bf16x8 vop[4];                               // V[16ks + 8hi + 0..7][32 ct + l32]
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) vop[ks] = kv.cols(Vl, 16 * ks, ct);
 
-    f32x16 O[2];
+    f32x16 O;
     if (!STATE_ONLY) {
       // ---- this wave's tiles of P^T, weighted
 #pragma unroll
@@ -183,52 +193,54 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
           f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ks = 0; ks < D / 32; ++ks)
-            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row8(Kl + Swizzled<D>::piece(16 * sb + l16, 4 * ks + q4)),
-                                                        lds_row8(Ql + Swizzled<D>::piece(16 * tb + l16, 4 * ks + q4)), x, 0, 0, 0);
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row8(Kl + Swizzled<D>::piece(16 * sb + l16, D / 32 * q4 + ks)),
+                                                        lds_row8(Ql + Swizzled<D>::piece(16 * tb + l16, D / 32 * q4 + ks)), x, 0, 0, 0);
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[r] = fac[i][r] != 0.f ? x[r] * fac[i][r] : 0.f;
           *reinterpret_cast<u32x2*>(Pl + Swizzled<C>::piece(16 * tb + l16, 2 * sb + (q4 >> 1)) + 4 * (q4 & 1)) =
               u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
         }
       }
-      // ---- S^T Q^T over this wave's rows of S, all queries
-      O[0] = f32x16{}; O[1] = f32x16{};
+    }
+    __builtin_amdgcn_sched_barrier(0);           // (the rest's reads ahead of the scores would cost registers)
+    // ---- S^T Q^T over this wave's rows of S: its own queries' and, for the other wave of the pair, that one's
+    bf16x8 sop[2 * G::IT];
+    if (!STATE_ONLY) {
 #pragma unroll
-      for (int it = 0; it < G::IT; ++it)
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const bf16x8 s = pack8(S[it], 8 * ks);
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) O[tt] = mfma(s, kv.rows(Ql, 32 * tt, 2 * (G::IT * half + it) + ks), O[tt]);
-        }
-      const f32x16 away = half ? O[0] : O[1];    // the other wave's queries
-      if (half) O[0] = O[1];
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4)
-        *reinterpret_cast<f32x4*>(Xl + (w * 4 + r4) * 256 + 4 * lane) = f32x4{away[4 * r4], away[4 * r4 + 1], away[4 * r4 + 2], away[4 * r4 + 3]};
+      for (int i = 0; i < 2 * G::IT; ++i) sop[i] = pack8(S[i / 2], 8 * (i % 2));
     }
     // ---- the state takes the group
-    const float keep = decay_pow(g2, n);
+    const float keep = n == C ? keep64 : decay_pow(g2, n);
 #pragma unroll
     for (int it = 0; it < G::IT; ++it) S[it] *= keep;
+    f32x16 away = {};
+    O = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
+      if (!STATE_ONLY && ks < 2 * G::IT) {
+        O = mfma(sop[ks], kv.rows(Ql, 32 * half, 2 * G::IT * half + ks), O);
+        away = mfma(sop[ks], kv.rows(Ql, 32 * (1 - half), 2 * G::IT * half + ks), away);
+      }
       f32x16 x;                                  // eight values; split8 and pack8 take them from an accumulator
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = 16 * ks + 8 * hi + j;
-        const float f = n == C ? fv[ks][j] : i < n ? decay_pow(g2, n - 1 - i) : 0.f;
-        x[j] = (float)vop[ks][j] * f;
-      }
+      for (int j = 0; j < 8; ++j) x[j] = (float)vop[ks][j] * fv[ks][j];
       bf16x8 vh, vo;
       if (TWO) split8(x, 0, vh, vo);
       else vh = pack8(x, 0);
+      bf16x8 k[G::IT];
 #pragma unroll
-      for (int it = 0; it < G::IT; ++it) {
-        const bf16x8 k = kx.cols(Kl, 16 * ks, G::IT * half + it);
-        S[it] = mfma(k, vh, S[it]);
-        if (TWO) S[it] = mfma(k, vo, S[it]);
+      for (int it = 0; it < G::IT; ++it) k[it] = kx.cols(Kl, 16 * ks, G::IT * half + it);
+#pragma unroll
+      for (int it = 0; it < G::IT; ++it) S[it] = mfma(k[it], vh, S[it]);
+      if (TWO) {
+#pragma unroll
+        for (int it = 0; it < G::IT; ++it) S[it] = mfma(k[it], vo, S[it]);
       }
+    }
+    if (!STATE_ONLY) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(Xl + (w * 4 + r4) * 256 + 4 * lane) = f32x4{away[4 * r4], away[4 * r4 + 1], away[4 * r4 + 2], away[4 * r4 + 3]};
     }
     if (!STATE_ONLY) {
       __syncthreads();                           // P; the read-outs from the other half's rows
@@ -237,15 +249,15 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
       for (int r4 = 0; r4 < 4; ++r4) {
         const f32x4 y = *reinterpret_cast<const f32x4*>(X + r4 * 256);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) O[0][4 * r4 + i] = (O[0][4 * r4 + i] + y[i]) * fq;
+        for (int i = 0; i < 4; ++i) O[4 * r4 + i] = (O[4 * r4 + i] + y[i]) * fq;
       }
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
-        if (ks < 2 || half) O[0] = mfma(vop[ks], pr.rows(Pl, 32 * half, ks), O[0]);
+        if (ks < 2 || half) O = mfma(vop[ks], pr.rows(Pl, 32 * half, ks), O);
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4)
         *reinterpret_cast<u32x2*>(Ol + Swizzled<D>::piece(32 * half + l32, 4 * ct + r4) + 4 * hi) =
-            u32x2{pack_bf16x2(O[0][4 * r4], O[0][4 * r4 + 1]), pack_bf16x2(O[0][4 * r4 + 2], O[0][4 * r4 + 3])};
+            u32x2{pack_bf16x2(O[4 * r4], O[4 * r4 + 1]), pack_bf16x2(O[4 * r4 + 2], O[4 * r4 + 3])};
     }
   }
   if (!STATE_ONLY) {
