@@ -65,4 +65,10 @@ __device__ __forceinline__ int clamp_len(const int32_t* lens, int b, int L) {
   return n < 0 ? 0 : n > L ? L : n;
 }
 
+// tokens of segment j of a sequence of len
+__device__ __forceinline__ int segment_tokens(int j, int seg_len, int len) {
+  const int left = len - j * seg_len;
+  return left < 0 ? 0 : left > seg_len ? seg_len : left;
+}
+
 }  // namespace linattn

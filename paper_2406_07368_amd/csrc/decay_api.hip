@@ -28,8 +28,7 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int dd) {
     for (int i = 0; i < 16; ++i)
       if (s0 + i < a.nseg) {
         p[(size_t)(s0 + i) * dd] = x;
-        const int left = len - (s0 + i) * a.seg_len, n = left < 0 ? 0 : left > a.seg_len ? a.seg_len : left;
-        x = decay_pow(g2, n) * x + inc[i];
+        x = decay_pow(g2, segment_tokens(s0 + i, a.seg_len, len)) * x + inc[i];
       }
   }
 }
@@ -41,7 +40,7 @@ __global__ __launch_bounds__(256) void state_through_kernel(const float* from, f
 
 // Up to so many segments every segment sums up for itself what those before it add (64 KB each at d = 128, from the L2 cache)
 // instead of a launch that does.
-constexpr int kFold = 8;
+constexpr int kFold = 4;
 
 struct Plan {
   int nseg, seg_len;
@@ -50,13 +49,14 @@ struct Plan {
 // A walk needs a compute unit (bf16 rows of 128: its two row buffers take 120 KB of LDS; rows of 64: half of one).
 // Where there are fewer walks the sequence is cut into segments of two groups or more, for one more read of K and V.
 Plan plan(const linattn_decay_desc* d, int32_t L, int roles) {
-  const int64_t walks = (int64_t)roles * d->B * d->H, room = d->d == 128 ? 256 : 512;
   Plan p{1, L, 0};
+  const bool f32 = d->io_dtype == LINATTN_F32;
+  const int64_t walks = (int64_t)roles * d->B * d->H, room = (d->d == 128 ? 256 : 512) * (f32 ? 2 : 1);
+  const int groups = (L + 63) / 64;
   int64_t n = room / walks;
-  if (n > L / 128) n = L / 128;
+  if (n > groups / (f32 ? 1 : 2)) n = groups / (f32 ? 1 : 2);
   if (n > 64) n = 64;
   if (n > 1) {
-    const int groups = (L + 63) / 64;
     p.seg_len = (int)((groups + n - 1) / n) * 64;
     p.nseg = (L + p.seg_len - 1) / p.seg_len;
     if (p.nseg > 1) p.bytes = (size_t)walks * p.nseg * d->d * d->d * sizeof(float);

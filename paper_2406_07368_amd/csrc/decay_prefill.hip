@@ -79,10 +79,9 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
   const int live_end = t_end < len ? t_end : len;                        // tokens that are there
   const int ng = live_end > t_begin ? (live_end - t_begin + C - 1) / C : 0;
   const Fetch<D, C, G::NT> fetch(tid);
-  auto buffer = [&](int i) { return smem + i * (STATE_ONLY ? 2 : 3) * G::TILE; };   // K, V, Q
-  auto request = [&](int gi) {
+  uint16_t *even = smem, *odd = smem + (STATE_ONLY ? 2 : 3) * G::TILE;   // K, V, Q
+  auto request = [&](int gi, uint16_t* buf) {
     const int tok0 = t_begin + gi * C, n = live_end - tok0;
-    uint16_t* buf = buffer(gi & 1);
     auto one = [&](uint16_t* to, const Walk& from) {
       if (reverse) fetch.template request<true>(to, from.p + (int64_t)(len - tok0 - (n < C ? n : C)) * from.t, from.t, n);
       else fetch.request(to, from.p + (int64_t)tok0 * from.t, from.t, n);
@@ -91,16 +90,15 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
     one(buf + G::TILE, wv);
     if (!STATE_ONLY) one(buf + 2 * G::TILE, wq);
   };
-  auto arrive = [&](int gi) {
+  auto arrive = [&](int gi, uint16_t* buf) {
     const int n = live_end - (t_begin + gi * C);
-    uint16_t* buf = buffer(gi & 1);
     fetch.arrived();
     fetch.trim(buf, n, tid);
     fetch.trim(buf + G::TILE, n, tid);
     if (!STATE_ONLY) fetch.trim(buf + 2 * G::TILE, n, tid);
     __syncthreads();
   };
-  if (ng > 0) request(0);
+  if (ng > 0) request(0, even);
 
   // ---- this wave's part of the state: register r of tile it is row 32 (G::IT half + it) + row_of(r), column 32 ct + l32
   auto row_of = [&](int r) { return 16 * (r >> 3) + 8 * hi + (r & 7); };
@@ -112,10 +110,9 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[it][r] = S0 ? S0[at(it, r)] : 0.f;
   if (!STATE_ONLY && a.nseg > 1 && a.fold) {     // few segments: what those before this one add, instead of a launch that sums it up
-    for (int j = 0; j < seg; ++j) {
+    for (int j = 0; j < seg; ++j) {              // (four increments in flight at once: 40 registers spilled, 8 % slower)
       const float* inc = a.ws + ((size_t)bhr * a.nseg + j) * (D * D);
-      const int left = len - j * a.seg_len, n = left < 0 ? 0 : left > a.seg_len ? a.seg_len : left;
-      const float keep = decay_pow(g2, n);
+      const float keep = decay_pow(g2, segment_tokens(j, a.seg_len, len));
 #pragma unroll
       for (int it = 0; it < G::IT; ++it)
 #pragma unroll
@@ -145,7 +142,7 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
 
   const float keep64 = decay_pow(g2, C);
   uint16_t* gout = const_cast<uint16_t*>(wo.p);
-  auto store_rows = [&](int gi) {
+  auto store_rows = [&](int gi, const uint16_t* Ol) {
     const int tok0 = t_begin + gi * C;
 #pragma unroll
     for (int i = 0; i < G::NP; ++i) {
@@ -159,16 +156,17 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
   // the tiles of P that are read but hold only later keys, (0, 1) and (2, 3), stay zeros
   if (!STATE_ONLY)
     for (int i = tid; i < C * C / 8; i += G::NT) *reinterpret_cast<u32x4*>(Pl + 8 * i) = u32x4{0u, 0u, 0u, 0u};
-  const Swizzled<D> kv(lane, 8), kx(lane, 8, true);
+  const Swizzled<D> kv0(lane, 8), kx0(lane, 8, true);
   const Swizzled<C> pr(lane, 8);
+  const int tile16 = Swizzled<D>::piece(l16, D / 32 * q4);   // a lane's piece of a 16-row operand; its ks-th: ^ (ks << 3)
 
-  for (int gi = 0; gi < ng; ++gi) {
+  auto group = [&](int gi, uint16_t* __restrict cur, uint16_t* __restrict next, uint16_t* __restrict Pl, float* __restrict Xl, uint16_t* __restrict Ol) {
     const int tok0 = t_begin + gi * C;
-    const uint16_t *Kl = buffer(gi & 1), *Vl = Kl + G::TILE, *Ql = Vl + G::TILE;
+    const uint16_t *Kl = cur, *Vl = Kl + G::TILE, *Ql = Vl + G::TILE;
     const int n = live_end - tok0 < C ? live_end - tok0 : C;
-    arrive(gi);                                  // the group's rows; the finished rows of the group before
-    if (gi + 1 < ng) request(gi + 1);
-    if (!STATE_ONLY && gi > 0) store_rows(gi - 1);
+    arrive(gi, cur);                             // the group's rows; the finished rows of the group before
+    if (gi + 1 < ng) request(gi + 1, next);
+    if (!STATE_ONLY && gi > 0) store_rows(gi - 1, Ol);
 
     if (n < C) {                                 // (the last group of all: the powers are not needed again)
 #pragma unroll
@@ -179,6 +177,11 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
           fv[ks][j] = i < n ? decay_pow(g2, n - 1 - i) : 0.f;
         }
     }
+    // (addresses kept over the loop would not fit the registers)
+    Swizzled<D> kv = kv0, kx = kx0;
+    kv.forget_rows(); kv.forget_cols(); kx.forget_cols();
+    int t16 = tile16;
+    asm volatile("" : "+v"(t16));
     bf16x8 vop[4];                               // V[16ks + 8hi + 0..7][32 ct + l32]
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) vop[ks] = kv.cols(Vl, 16 * ks, ct);
@@ -193,8 +196,8 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
           f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ks = 0; ks < D / 32; ++ks)
-            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row8(Kl + Swizzled<D>::piece(16 * sb + l16, D / 32 * q4 + ks)),
-                                                        lds_row8(Ql + Swizzled<D>::piece(16 * tb + l16, D / 32 * q4 + ks)), x, 0, 0, 0);
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row8(Kl + 16 * sb * D + (t16 ^ (ks << 3))),
+                                                        lds_row8(Ql + 16 * tb * D + (t16 ^ (ks << 3))), x, 0, 0, 0);
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[r] = fac[i][r] != 0.f ? x[r] * fac[i][r] : 0.f;
           *reinterpret_cast<u32x2*>(Pl + Swizzled<C>::piece(16 * tb + l16, 2 * sb + (q4 >> 1)) + 4 * (q4 & 1)) =
@@ -259,11 +262,15 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
         *reinterpret_cast<u32x2*>(Ol + Swizzled<D>::piece(32 * half + l32, 4 * ct + r4) + 4 * hi) =
             u32x2{pack_bf16x2(O[4 * r4], O[4 * r4 + 1]), pack_bf16x2(O[4 * r4 + 2], O[4 * r4 + 3])};
     }
+  };
+  for (int gi = 0; gi < ng; gi += 2) {           // (two at a time: the buffers' addresses are constants.  __restrict: see Fetch)
+    group(gi, even, odd, Pl, Xl, Ol);
+    if (gi + 1 < ng) group(gi + 1, odd, even, Pl, Xl, Ol);
   }
   if (!STATE_ONLY) {
     if (ng > 0) {
       __syncthreads();
-      store_rows(ng - 1);
+      store_rows(ng - 1, Ol);
     }
     // rows behind the end of the sequence, in groups that the walk has not met
     for (int e = tid; e < (t_end - t_begin - ng * C) * G::PPR; e += G::NT) {

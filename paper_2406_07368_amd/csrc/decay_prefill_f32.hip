@@ -9,6 +9,7 @@
 #include "common.h"
 #include "decay.h"
 #include "kernels.h"
+#include "swizzle.h"
 
 namespace linattn {
 
@@ -67,8 +68,7 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
   if (!STATE_ONLY && a.nseg > 1 && a.fold) {
     for (int j = 0; j < seg; ++j) {
       const float* inc = a.ws + ((size_t)bhr * a.nseg + j) * (D * D);
-      const int left = len - j * a.seg_len, n = left < 0 ? 0 : left > a.seg_len ? a.seg_len : left;
-      const float keep = decay_pow(g2, n);
+      const float keep = decay_pow(g2, segment_tokens(j, a.seg_len, len));
 #pragma unroll
       for (int it = 0; it < G::RT; ++it)
 #pragma unroll
@@ -118,6 +118,13 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
     __syncthreads();
     if (gi + 1 < ng) request(tok0 + C);
 
+    if (n < C) {                              // (the last group of all: the powers are not needed again)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = acc_row(r, hi);
+        fv[r] = i < n ? decay_pow(g2, n - 1 - i) : 0.f;
+      }
+    }
     f32x16 O = {};
     if (!STATE_ONLY) {
       // ---- this wave's part of P^T: 32 features, of which a half of the wave takes 16
@@ -151,13 +158,12 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
     const float keep = decay_pow(g2, n);
 #pragma unroll
     for (int it = 0; it < G::RT; ++it) S[it] *= keep;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int i = acc_row(r, hi);
-      const float f = n == C ? fv[r] : i < n ? decay_pow(g2, n - 1 - i) : 0.f;
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
-      for (int it = 0; it < G::RT; ++it) S[it] = mfma_f32(Kl[i * G::RS + 32 * it + l32], v[r] * f, S[it]);
-    }
+      for (int it = 0; it < G::RT; ++it) S[it] = mfma_f32(Kl[acc_row(r, hi) * G::RS + 32 * it + l32], v[r] * fv[r], S[it]);
+    read_ahead<8, 1, 1, 16 * G::RT>();
     if (!STATE_ONLY) {
       __syncthreads();                      // the parts of P; every wave is done with the Q rows
 #pragma unroll

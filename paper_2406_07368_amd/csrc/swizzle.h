@@ -27,6 +27,10 @@ struct Swizzled {
     const int r = order * hi + (j >> 2), c4 = crossed ? ((j & 1) << 1) | ((j >> 1) & 1) : j & 3;
     tr = piece(r, 2 * ((lane >> 4) & 1) + (c4 >> 1)) + 4 * (c4 & 1);
   }
+  // From here on the compiler does not know the offsets: it makes the addresses that hang on them anew where they are used
+  // instead of keeping them in registers over a loop.
+  __device__ __forceinline__ void forget_rows() { asm volatile("" : "+v"(row)); }
+  __device__ __forceinline__ void forget_cols() { asm volatile("" : "+v"(tr)); }
   // lanes <-> rows row0 + 0..31 (a multiple of 32), registers <-> elements 16 ks + 8 (lane / 32) + 0..7
   __device__ __forceinline__ bf16x8 rows(const uint16_t* base, int row0, int ks) const { return lds_row8(base + row0 * D + (row ^ (ks << 4))); }
   // lanes <-> elements 32 ct + lane % 32, registers <-> rows row0 + 0..15 (a multiple of 16) in an accumulator's order ...
@@ -43,22 +47,26 @@ struct Swizzled {
   }
 };
 
-// For a run of N products whose operands (one LDS read each) the compiler would fetch one by one, each product waiting for its
-// own: the first A reads, then product and read in turn.
-template <int A, int N>
+// For a run of N products whose operands (R LDS reads for every M of them) the compiler would fetch one by one, each product
+// waiting for its own: A reads first, then M products and R reads in turn.
+template <int A, int R, int M, int N>
 __device__ __forceinline__ void read_ahead() {
   __builtin_amdgcn_sched_group_barrier(0x100, A, 0);      // LDS reads
+  constexpr int turns = (N / M * R - A + R - 1) / R;
 #pragma unroll
-  for (int i = 0; i < N - A; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // MFMA
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  for (int i = 0; i < turns; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);    // MFMA
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+  __builtin_amdgcn_sched_group_barrier(0x008, N - turns * M, 0);
 }
 
 // ROWS rows of D bf16 from memory straight into LDS, NT threads: a wave's request fills 1 KB in the order of its lanes, so a
 // lane asks for the piece that belongs at its place.  `rows` of them are there: the others re-read row 0 and are overwritten
 // with zeros (by the thread that asked for them) once they are in.
+// The caller waits: arrived(), then a barrier.  Between a request and that the compiler must know that what the code reads by
+// transposed operands and what it writes is not what is under way, or it waits there and then: the buffers are __restrict
+// parameters of whatever holds both.
 template <int D, int ROWS = 64, int NT = 256>
 struct Fetch {
   static constexpr int PPR = D / 8, NP = ROWS * PPR / NT, RP = NT / PPR;   // (RP rows on: the same permutation)

@@ -15,7 +15,7 @@ struct WindowArgs {
   Rows dout, dq, dk, dv;          // gradient
   const int32_t* lens;
   float* lse;                     // [B,H,L]: written by the prefill (may be null), read by the gradient
-  float* delta;                   // gradient: [B,H,L], dout . out
+  float* stats;                   // gradient: [2][B,H,L], lse in base 2 and dout . out
   int far;                        // gradient: workgroups per key/value head for the queries that see only sinks of key tile 0
   int parts;                      // gradient: workgroups per key tile
   float* sink_part;               // far > 0: [B*H_kv][parts + 2 far][2][sinks][d], shares of the sinks' dk, dv

@@ -67,7 +67,7 @@ GradientPlan plan_gradient(const linattn_window_desc* d, int32_t L) {
     if (n > (items + 3) / 4) n = (items + 3) / 4;
     p.far = (int)n;
   }
-  p.off_sinks = round256((size_t)d->B * d->H * L * sizeof(float));
+  p.off_sinks = round256(2 * (size_t)d->B * d->H * L * sizeof(float));
   p.off_part = p.off_sinks + round256(p.far ? (size_t)heads * (p.parts + 2 * p.far) * 2 * d->sinks * d->d * sizeof(float) : 0);
   p.bytes = p.off_part + (p.parts > 1 ? (size_t)heads * p.parts * 2 * L * d->d * sizeof(float) : 0);
   return p;
@@ -122,7 +122,7 @@ linattn_status linattn_window_backward(const linattn_window_desc* desc, int32_t 
   a.out = rows(out, desc->out); a.dout = rows(dout, desc->dout);
   a.dq = rows(dq, desc->dq); a.dk = rows(dk, desc->dk); a.dv = rows(dv, desc->dv);
   a.lse = const_cast<float*>(lse);
-  a.delta = static_cast<float*>(workspace);
+  a.stats = static_cast<float*>(workspace);
   a.sink_part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_sinks);
   a.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
   a.far = p.far; a.parts = p.parts;

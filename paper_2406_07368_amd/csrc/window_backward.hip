@@ -7,7 +7,7 @@
 // products of 2 d flops a visible pair where five would do).
 //   rows of q    128 queries a workgroup, a wave's 32 in its lanes, keys 64 at a time through LDS, as in the prefill:
 //                S^T = K Q^T, dP^T = V dO^T, and dS^T, packed, is the operand of dQ^T += K^T dS^T as it stands.  Writes
-//                delta for the other kernel.
+//                lse (in base 2) and delta for the other kernel.
 //   rows of k, v 128 keys of a key/value head a workgroup, a wave's 32 in its lanes, queries 32 at a time through LDS,
 //                over all query heads that share the keys: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  The
 //                value rows stay in LDS and not in registers, so that two waves fit a SIMD.
@@ -105,8 +105,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
     }
   }
   delta = add_xor32(delta);
-  if (hi == 0 && t < len) a.delta[stat + t] = delta;
   const float lse2 = a.lse[stat + tr] * 1.44269504088896340736f;
+  if (t < len) a.stats[hi * (int64_t)a.B * a.H * a.L + stat + t] = hi ? delta : lse2;
 
   const int last = (t_end < len ? t_end : len) - 1;
   const int lo = (t0 - a.window + 1 > 0 ? t0 - a.window + 1 : 0) / 64;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
         x = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x);
         y = mfma(lds.rows(Vl, 32 * kt, ks), dop[ks], y);
       }
-      read_ahead<6, 2 * G::KS>();
+      read_ahead<6, 1, 1, 2 * G::KS>();
       const bool all = sw + 31 <= tw && (sw > tw + 31 - a.window || sw + 32 <= a.sinks);
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r] * c - lse2) * (y[r] - delta);
@@ -158,16 +158,16 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
       }
     }
   };
+  auto turn = [&](int i, uint16_t* __restrict cur, uint16_t* __restrict next) {   // (see Fetch)
+    arrive(i, cur);
+    if (i + 1 < nk) request(i + 1, next);
+    tile_of(i, cur);
+  };
   uint16_t *even = smem, *odd = smem + G::BUF;
   request(0, even);
   for (int i = 0; i < nk; i += 2) {
-    arrive(i, even);
-    if (i + 1 < nk) request(i + 1, odd);
-    tile_of(i, even);
-    if (i + 1 >= nk) break;
-    arrive(i + 1, odd);
-    if (i + 2 < nk) request(i + 2, even);
-    tile_of(i + 1, odd);
+    turn(i, even, odd);
+    if (i + 1 < nk) turn(i + 1, odd, even);
   }
   store_tile<D>(smem, dQ, a.scale, gdq, a.dq.t, t0, t_end, len, tid);
 }
@@ -231,23 +231,22 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
   const int items = q_n * group;
 
   const Fetch<D, kWindowQ> fetch(tid);
-  float rs = 0.f;
   auto first_row = [&](int it) { return (q_lo + it % q_n) * kWindowQ; };
-  auto request = [&](int it, uint16_t* buf) {
+  auto request = [&](int it, uint16_t* buf, float* st) {
     const int h = hk * group + it / q_n, t0 = first_row(it), n = len - t0;
     fetch.request(buf, static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h + t0 * a.q.t, a.q.t, n);
     fetch.request(buf + kWindowQ * D, static_cast<const uint16_t*>(a.dout.p) + b * a.dout.b + h * a.dout.h + t0 * a.dout.t, a.dout.t, n);
-    if (tid < 2 * kWindowQ) {
-      const int64_t at = ((int64_t)b * a.H + h) * a.L + t0 + tid % kWindowQ;
-      rs = tid % kWindowQ < n ? (tid < kWindowQ ? a.lse[at] * 1.44269504088896340736f : a.delta[at]) : 0.f;
+    if (w == 0) {                                // lanes: lse in base 2, then delta (behind the end: the last token's)
+      const int r = lane % kWindowQ < n ? lane % kWindowQ : n - 1;
+      const float* from = a.stats + (lane < kWindowQ ? 0 : (int64_t)a.B * a.H * a.L) + ((int64_t)b * a.H + h) * a.L + t0 + r;
+      __builtin_amdgcn_global_load_lds((typename Fetch<D>::global_ptr)from, (typename Fetch<D>::lds_ptr)st, 4, 0, 0);
     }
   };
-  auto arrive = [&](int it, uint16_t* buf, float* st) {
+  auto arrive = [&](int it, uint16_t* buf) {
     const int n = len - first_row(it);
     fetch.arrived();
     fetch.trim(buf, n, tid);
     fetch.trim(buf + kWindowQ * D, n, tid);
-    if (tid < 2 * kWindowQ) st[tid] = rs;
     __syncthreads();
   };
 
@@ -259,11 +258,16 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
     const int tw = first_row(it);
     if (sink_job ? (turn & 1) != w >> 1 || kw >= a.sinks : !(kw <= tw + 31 && (kw + 31 > tw - a.window || kw < a.sinks))) return;
     f32x16 x = {}, y = {};
+    int vo = (kw - s0) * D;
+    Swizzled<D> at = lds;                        // (addresses kept over the loop would not fit the registers)
+    asm volatile("" : "+s"(vo));
+    at.forget_rows();
 #pragma unroll
     for (int ks = 0; ks < G::KS; ++ks) {
-      x = mfma(lds.rows(Ql, 0, ks), kop[ks], x);
-      y = mfma(lds.rows(dl, 0, ks), lds.rows(Vl, kw - s0, ks), y);
+      x = mfma(at.rows(Ql, 0, ks), kop[ks], x);
+      y = mfma(at.rows(dl, 0, ks), at.rows(Vl + vo, 0, ks), y);
     }
+    if constexpr (D == 128) read_ahead<9, 3, 2, 16>();
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
       const f32x4 le = *reinterpret_cast<const f32x4*>(st + 8 * r4 + 4 * hi);
@@ -282,29 +286,31 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
         if (!(window_sees(t, s, a.window, a.sinks) && t < len)) { x[r] = 0.f; y[r] = 0.f; }
       }
     }
+    at.forget_cols();
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const bf16x8 p = pack8(x, 8 * half), ds = pack8(y, 8 * half);
 #pragma unroll
       for (int ct = 0; ct < G::CT; ++ct) {
-        dV[ct] = mfma(lds.cols_acc(dl, 16 * half, ct), p, dV[ct]);
-        dK[ct] = mfma(lds.cols_acc(Ql, 16 * half, ct), ds, dK[ct]);
+        dV[ct] = mfma(at.cols_acc(dl, 16 * half, ct), p, dV[ct]);
+        dK[ct] = mfma(at.cols_acc(Ql, 16 * half, ct), ds, dK[ct]);
       }
     }
+    if constexpr (D == 128) read_ahead<4, 2, 1, 16>();
   };
   uint16_t *even = smem + 128 * D, *odd = even + 2 * kWindowQ * D;
-  if (part < items) request(part, even);
+  if (part < items) request(part, even, stats);
   vfetch.arrived();
 #pragma unroll
   for (int i = 0; i < 2; ++i) vfetch.trim(Vl + i * 64 * D, len - s0 - 64 * i, tid);
+  auto one = [&](int it, int turn, uint16_t* __restrict cur, float* __restrict st, uint16_t* __restrict next, float* __restrict st_next) {
+    arrive(it, cur);
+    if (it + step < items) request(it + step, next, st_next);
+    tile_of(it, turn, cur, st);
+  };
   for (int it = part, turn = 0; it < items; it += 2 * step, turn += 2) {
-    arrive(it, even, stats);
-    if (it + step < items) request(it + step, odd);
-    tile_of(it, turn, even, stats);
-    if (it + step >= items) break;
-    arrive(it + step, odd, stats + 2 * kWindowQ);
-    if (it + 2 * step < items) request(it + 2 * step, even);
-    tile_of(it + step, turn + 1, odd, stats + 2 * kWindowQ);
+    one(it, turn, even, stats, odd, stats + 2 * kWindowQ);
+    if (it + step < items) one(it + step, turn + 1, odd, stats + 2 * kWindowQ, even, stats);
   }
   if (!sink_job && a.parts == 1) {
     store_tile<D>(smem, dK, a.scale, gdk, a.dk.t, s0, s_end, len, tid);

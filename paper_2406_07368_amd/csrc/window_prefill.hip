@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) x[kt] = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x[kt]);
-    read_ahead<6, D / 8>();
+    read_ahead<6, 1, 1, D / 8>();
     const bool all = s0 + KT - 1 <= tw && (s0 > tw + 31 - a.window || s0 + KT <= a.sinks);
     if (!all) {
 #pragma unroll
@@ -144,16 +144,16 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
         for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(lds.cols_acc(Vl, 32 * kt + 16 * half, ct), p, O[ct]);
       }
   };
+  auto turn = [&](int i, uint16_t* __restrict cur, uint16_t* __restrict next) {   // (see Fetch)
+    arrive(i, cur);
+    if (i + 1 < nk) request(i + 1, next);
+    tile_of(i, cur);
+  };
   uint16_t *even = smem, *odd = smem + G::BUF;
   request(0, even);
   for (int i = 0; i < nk; i += 2) {             // (two at a time: the buffers' addresses are constants)
-    arrive(i, even);
-    if (i + 1 < nk) request(i + 1, odd);
-    tile_of(i, even);
-    if (i + 1 >= nk) break;
-    arrive(i + 1, odd);
-    if (i + 2 < nk) request(i + 2, even);
-    tile_of(i + 1, odd);
+    turn(i, even, odd);
+    if (i + 1 < nk) turn(i + 1, odd, even);
   }
 
   l = add_xor32(l);
