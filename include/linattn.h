@@ -379,8 +379,9 @@ size_t linattn_decay_backward_workspace_bytes(const linattn_decay_desc *desc, in
  *   q, k, v      in   [B,H,L,d] by strides;  out  out  [B,H,L,d] by strides
  *   S_in         in, optional   float [B,H,d,d] dense (row = key feature), NULL = zeros
  *   S_out        out, optional  the state after lens[b] tokens; may be S_in
- * bf16 rows: matrix cores, fp32 accumulation; in-group weights and the state's read-out are rounded to bf16 once,
- * and what enters the state carries sixteen significant bits.  fp32 rows: exact fp32 products. */
+ * bf16 rows: matrix cores, fp32 accumulation; in-group weights and the state's read-out are rounded to bf16 once.
+ * The state takes fp32 products where it is handed back, else sixteen significant bits of them.  fp32 rows: exact
+ * fp32 products. */
 linattn_status linattn_decay_prefill(const linattn_decay_desc *desc, int32_t L,
                                      const void *q, const void *k, const void *v,
                                      const float *log_decay, const int32_t *lens,

@@ -30,7 +30,6 @@ struct DecayArgs {
   int nseg, seg_len;       // segments of seg_len tokens (a multiple of 64), in the order of the walk
   int fold;                // few segments: the workspace holds what each adds, and each sums up those before it
   float scale;
-  int exact_state;         // what enters the state carries sixteen significant bits (else eight: the gradient's own states)
 };
 hipError_t launch_decay_first_pass_bf16(const DecayArgs& a, int d, hipStream_t s);
 hipError_t launch_decay_rows_bf16(const DecayArgs& a, int d, hipStream_t s);
@@ -53,6 +52,12 @@ hipError_t launch_decay_step(const DecayStepArgs& a, int d, bool bf16, hipStream
 __device__ __forceinline__ float decay_log2(const float* log_decay, int h) {
   const float g = log_decay[h] * 1.44269504088896340736f;
   return g < 0.f ? fmaxf(g, -1e30f) : 0.f;
+}
+// lambda^n - 1, n >= 0, for a state that decays by it once a group: x + x (lambda^n - 1).  A factor near 1 held as such is off by
+// 2^-24, always to the same side, and a slow head's state meets it dozens of times.
+__device__ __forceinline__ float decay_pow_less_1(const float* log_decay, int h, int n) {
+  const float g = log_decay[h];
+  return g < 0.f ? expm1f(fmaxf(g, -1e30f) * (float)n) : 0.f;
 }
 // lambda^n, n >= 0
 __device__ __forceinline__ float decay_pow(float g2, int n) { return __builtin_amdgcn_exp2f(g2 * (float)n); }

@@ -128,7 +128,7 @@ linattn_status linattn_decay_prefill(const linattn_decay_desc* desc, int32_t L, 
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return LINATTN_ERR_WORKSPACE;
   DecayArgs a{};
   a.role[0] = {rows(q, desc->q), rows(k, desc->k), rows(v, desc->v), rows(out, desc->out), 0};
-  a.roles = 1; a.L = L; a.log_decay = log_decay; a.lens = lens; a.S_in = S_in; a.S_out = S_out; a.exact_state = 1;
+  a.roles = 1; a.L = L; a.log_decay = log_decay; a.lens = lens; a.S_in = S_in; a.S_out = S_out;
   return run(a, desc, p, workspace, s);
 }
 

@@ -14,8 +14,9 @@
 // read); it reads for all 64 tokens and gives the other wave of the pair, through LDS, what that one's tokens get from its
 // rows.  The scores are ten 16 x 16 tiles, dealt out over the waves.  Rows come straight into one of two LDS buffers while
 // the other is worked on (swizzle.h); finished rows leave through LDS, so that whole rows are stored.
-// V' enters the state as the sum of two bf16 terms (sixteen significant bits: S is handed back in fp32 and lives on in
-// generation); where the state is only this launch's own (the gradient) one term is enough.
+// V' enters the state as the sum of TERMS bf16 terms.  Two carry sixteen significant bits: with one, the gradient's error was
+// 1.65 times that of the final rounding alone, with two it is 1.4 times.  A state that is handed back in fp32 takes three, all
+// of an fp32 product's bits (its error at LLaMA size: 3.6e-7, with two terms 2.5e-6, for 275 us in the place of 256).
 //
 // The gradient is the same function with other roles: dq = F(dout, v, k), and over reversed time dk = F(v, dout, q),
 // dv = F(k, q, dout); a launch carries up to three roles.
@@ -54,7 +55,7 @@ __device__ __forceinline__ Walk walk(const Rows& r, int b, int h) {
   return {static_cast<const uint16_t*>(r.p) + b * r.b + h * r.h, r.t};
 }
 
-template <int D, bool STATE_ONLY, bool TWO>
+template <int D, bool STATE_ONLY, int TERMS>
 __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs a) {
   using G = Cfg<D>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
 #pragma unroll
     for (int j = 0; j < 8; ++j) fv[ks][j] = decay_pow(g2, 63 - (16 * ks + 8 * hi + j));
 
-  const float keep64 = decay_pow(g2, C);
+  const float less64 = decay_pow_less_1(a.log_decay, h, C);
   uint16_t* gout = const_cast<uint16_t*>(wo.p);
   auto store_rows = [&](int gi, const uint16_t* Ol) {
     const int tok0 = t_begin + gi * C;
@@ -213,9 +214,10 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
       for (int i = 0; i < 2 * G::IT; ++i) sop[i] = pack8(S[i / 2], 8 * (i % 2));
     }
     // ---- the state takes the group
-    const float keep = n == C ? keep64 : decay_pow(g2, n);
+    float less = less64;
+    if (n < C) less = decay_pow_less_1(a.log_decay, h, n);
 #pragma unroll
-    for (int it = 0; it < G::IT; ++it) S[it] *= keep;
+    for (int it = 0; it < G::IT; ++it) S[it] += S[it] * less;
     f32x16 away = {};
     O = f32x16{};
 #pragma unroll
@@ -224,21 +226,23 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
         O = mfma(sop[ks], kv.rows(Ql, 32 * half, 2 * G::IT * half + ks), O);
         away = mfma(sop[ks], kv.rows(Ql, 32 * (1 - half), 2 * G::IT * half + ks), away);
       }
-      f32x16 x;                                  // eight values; split8 and pack8 take them from an accumulator
+      f32x16 x;                                  // eight values; split8 takes them from an accumulator
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = (float)vop[ks][j] * fv[ks][j];
-      bf16x8 vh, vo;
-      if (TWO) split8(x, 0, vh, vo);
-      else vh = pack8(x, 0);
+      bf16x8 vt[3];
+      split8(x, 0, vt[0], vt[1]);
+      if (TERMS == 3) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = x[j] - (float)vt[0][j] - (float)vt[1][j];
+        vt[2] = pack8(x, 0);
+      }
       bf16x8 k[G::IT];
 #pragma unroll
       for (int it = 0; it < G::IT; ++it) k[it] = kx.cols(Kl, 16 * ks, G::IT * half + it);
 #pragma unroll
-      for (int it = 0; it < G::IT; ++it) S[it] = mfma(k[it], vh, S[it]);
-      if (TWO) {
+      for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-        for (int it = 0; it < G::IT; ++it) S[it] = mfma(k[it], vo, S[it]);
-      }
+        for (int it = 0; it < G::IT; ++it) S[it] = mfma(k[it], vt[i], S[it]);
     }
     if (!STATE_ONLY) {
 #pragma unroll
@@ -287,25 +291,25 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
   }
 }
 
-template <int D, bool STATE_ONLY, bool TWO>
+template <int D, bool STATE_ONLY, int TERMS>
 hipError_t launch(const DecayArgs& a, hipStream_t s) {
   using G = Cfg<D>;
   constexpr int bytes = STATE_ONLY ? G::KV : G::ALL;
-  hipError_t e = LINATTN_MAX_LDS_ONCE((decay_prefill_kernel<D, STATE_ONLY, TWO>), bytes);
+  hipError_t e = LINATTN_MAX_LDS_ONCE((decay_prefill_kernel<D, STATE_ONLY, TERMS>), bytes);
   if (e != hipSuccess) return e;
-  decay_prefill_kernel<D, STATE_ONLY, TWO><<<dim3(a.roles * a.B * a.H * a.nseg), G::NT, bytes, s>>>(a);
+  decay_prefill_kernel<D, STATE_ONLY, TERMS><<<dim3(a.roles * a.B * a.H * a.nseg), G::NT, bytes, s>>>(a);
   return hipGetLastError();
+}
+
+template <bool STATE_ONLY>
+hipError_t launch_d(const DecayArgs& a, int d, hipStream_t s) {
+  if (a.S_out) return d == 64 ? launch<64, STATE_ONLY, 3>(a, s) : launch<128, STATE_ONLY, 3>(a, s);
+  return d == 64 ? launch<64, STATE_ONLY, 2>(a, s) : launch<128, STATE_ONLY, 2>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_decay_first_pass_bf16(const DecayArgs& a, int d, hipStream_t s) {
-  if (d == 64) return a.exact_state ? launch<64, true, true>(a, s) : launch<64, true, false>(a, s);
-  return a.exact_state ? launch<128, true, true>(a, s) : launch<128, true, false>(a, s);
-}
-hipError_t launch_decay_rows_bf16(const DecayArgs& a, int d, hipStream_t s) {
-  if (d == 64) return a.exact_state ? launch<64, false, true>(a, s) : launch<64, false, false>(a, s);
-  return a.exact_state ? launch<128, false, true>(a, s) : launch<128, false, false>(a, s);
-}
+hipError_t launch_decay_first_pass_bf16(const DecayArgs& a, int d, hipStream_t s) { return launch_d<true>(a, d, s); }
+hipError_t launch_decay_rows_bf16(const DecayArgs& a, int d, hipStream_t s) { return launch_d<false>(a, d, s); }
 
 }  // namespace linattn

@@ -84,6 +84,7 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
     fv[r] = decay_pow(g2, C - 1 - acc_row(r, hi));
   }
   const float fq = decay_pow(g2, l32 + 1) * a.scale;
+  const float less32 = decay_pow_less_1(a.log_decay, h, C);
 
   f32x4 rq[G::NP], rk[G::NP], rv[G::NP];
   auto request = [&](int tok0) {
@@ -155,9 +156,10 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
     float v[16];                            // V[acc_row(r)][c0 + l32]
 #pragma unroll
     for (int r = 0; r < 16; ++r) v[r] = Vl[acc_row(r, hi) * G::RS + c0 + l32];
-    const float keep = decay_pow(g2, n);
+    float less = less32;
+    if (n < C) less = decay_pow_less_1(a.log_decay, h, n);
 #pragma unroll
-    for (int it = 0; it < G::RT; ++it) S[it] *= keep;
+    for (int it = 0; it < G::RT; ++it) S[it] += S[it] * less;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int r = 0; r < 16; ++r)

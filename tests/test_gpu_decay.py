@@ -15,7 +15,7 @@ BF, F32 = torch.bfloat16, torch.float32
 # d + 64 products in a row and one addition per group.
 ROUNDINGS = {BF: 2, F32: 200}
 NORM = {BF: None, F32: 5e-6}                     # fp32: the errors of a few hundred additions, random in sign
-STATE_BITS = 2.0 ** -16                          # bf16 rows: 2^-17 of each product that enters, and fp32 sums
+STATE_BITS = 2.0 ** -18                          # products of 24 bits, fp32 sums
 
 
 def rows(B, H, L, d, dtype, seed, n=3, scale=1.0):
@@ -31,8 +31,8 @@ def cuda(*xs):
     return [None if x is None else x.cuda() for x in xs]
 
 
-def check_state(S, want, size, dtype, what):
-    off = (S.double().cpu() - want).abs() - (STATE_BITS if dtype == BF else 2.0 ** -18) * size - 1e-30
+def check_state(S, want, size, what):
+    off = (S.double().cpu() - want).abs() - STATE_BITS * size - 1e-30
     assert float(off.max()) <= 0, what
 
 
@@ -50,7 +50,10 @@ def test_prefill(dtype, B, H, L, d, state, ragged):
     a = cuda(q, k, v, g, S0, lens)
     out, Sg = binding.decay_prefill(a[0], a[1], a[2], a[3], 0.25, a[4], a[5])
     near(out, want, size, dtype, ROUNDINGS[dtype], "out", NORM[dtype])
-    check_state(Sg, S, A, dtype, "S")
+    check_state(Sg, S, A, "S")
+    alone, none = binding.decay_prefill(a[0], a[1], a[2], a[3], 0.25, a[4], a[5], want_state=False)
+    assert none is None
+    near(alone, want, size, dtype, ROUNDINGS[dtype], "out without the state", NORM[dtype])
     if lens is not None:
         behind = torch.arange(L) >= lens[:, None]
         assert not out.cpu().float().transpose(1, 2)[behind].any()
@@ -82,7 +85,7 @@ def test_decays_at_the_ends_of_their_range(dtype):
     a = cuda(q, k, v, g)
     out, Sg = binding.decay_prefill(*a, 1.0)
     near(out, want, size, dtype, ROUNDINGS[dtype], "out", NORM[dtype])
-    check_state(Sg, S, A, dtype, "S")
+    check_state(Sg, S, A, "S")
     S1 = torch.zeros_like(Sg)
     steps = [binding.decay_step(*[x[:, :, t:t + 8].contiguous() for x in a[:3]], a[3], S1, 1.0) for t in range(0, 200, 8)]
     near(torch.cat(steps, 2), want, size, dtype, ROUNDINGS[dtype], "steps", NORM[dtype])
