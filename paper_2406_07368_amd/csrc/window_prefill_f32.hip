@@ -1,10 +1,10 @@
 // Softmax attention over a sliding window with sinks, fp32 rows, in exact fp32 products (v_mfma_f32_32x32x2_f32).  The
-// scheme is window_prefill.hip's with 32 keys at a time: 128 queries a workgroup, 32 a wave, a query per lane, one pass
+// scheme is window_prefill.hip's with 32 keys at a time: 128 or 64 queries a workgroup, 32 a wave, a query per lane, one pass
 // with a running maximum and sum.  A register of the score accumulator holds the keys s (low half of the wave) and s + 4
 // (high half), which is an operand of the fp32 instruction as it stands: the weights move nowhere.  The two halves of a
 // wave contract the two halves of the features.
 //
-// Bound: the fp32 matrix rate (4 d flops a visible pair).
+// Bound: the fp32 matrix rate (4 d flops a visible pair): 97 TFLOP/s at 64 heads of 4096 tokens, d = 128, a window of 1024.
 #include "common.h"
 #include "kernels.h"
 #include "window.h"
@@ -13,21 +13,22 @@ namespace linattn {
 
 namespace {
 
-constexpr int QT = 128, KT = 32;
+constexpr int KT = 32;
 
-template <int D>
+template <int D, int QT>
 struct Cfg {
+  static constexpr int NT = 2 * QT;              // a wave for 32 queries
   static constexpr int RS = D + 4;
   static constexpr int PPR = D / 4;
-  static constexpr int NP = KT * PPR / 256;
+  static constexpr int NP = KT * PPR / NT;
   static constexpr int FLOATS = QT * RS > 2 * KT * RS ? QT * RS : 2 * KT * RS;   // finished rows; K, V
 };
 
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a) {
-  using G = Cfg<D>;
+template <int D, int QT>
+__global__ __launch_bounds__(2 * QT, 2) void window_prefill_f32_kernel(WindowArgs a) {
+  using G = Cfg<D, QT>;
   extern __shared__ __attribute__((aligned(16))) float smem_f[];
   const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
   const int place = xcd_place(blockIdx.x, a.B * a.Hkv, group * ntile);
@@ -43,9 +44,9 @@ __global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a
   float* glse = a.lse ? a.lse + ((int64_t)b * a.H + h) * a.L : nullptr;
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
   if (t0 >= len) {
-    for (int e = tid; e < (t_end - t0) * G::PPR; e += 256) *reinterpret_cast<f32x4*>(gout + (t0 + e / G::PPR) * a.out.t + e % G::PPR * 4) = z;
+    for (int e = tid; e < (t_end - t0) * G::PPR; e += G::NT) *reinterpret_cast<f32x4*>(gout + (t0 + e / G::PPR) * a.out.t + e % G::PPR * 4) = z;
     if (glse)
-      for (int t = t0 + tid; t < t_end; t += 256) glse[t] = -__builtin_inff();
+      for (int t = t0 + tid; t < t_end; t += G::NT) glse[t] = -__builtin_inff();
     return;
   }
   const float* gq = static_cast<const float*>(a.q.p) + b * a.q.b + h * a.q.h;
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a
   auto request = [&](int s0) {
 #pragma unroll
     for (int i = 0; i < G::NP; ++i) {
-      const int p = tid + 256 * i, s = s0 + p / G::PPR, e = p % G::PPR * 4;
+      const int p = tid + G::NT * i, s = s0 + p / G::PPR, e = p % G::PPR * 4;
       const int row = s < len ? s : 0;
       rk[i] = *reinterpret_cast<const f32x4*>(gk + row * a.k.t + e);
       rv[i] = *reinterpret_cast<const f32x4*>(gv + row * a.v.t + e);
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < G::NP; ++j) {
-      const int p = tid + 256 * j;
+      const int p = tid + G::NT * j;
       float* d = Kl + p / G::PPR * G::RS + p % G::PPR * 4;
       const bool in = s0 + p / G::PPR < len;
       *reinterpret_cast<f32x4*>(d) = in ? rk[j] : z;
@@ -148,23 +149,28 @@ __global__ __launch_bounds__(256, 2) void window_prefill_f32_kernel(WindowArgs a
     }
   __syncthreads();
 #pragma unroll 4
-  for (int i = 0; i < QT * G::PPR / 256; ++i) {
-    const int p = tid + 256 * i, r = p / G::PPR;
+  for (int i = 0; i < QT * G::PPR / G::NT; ++i) {
+    const int p = tid + G::NT * i, r = p / G::PPR;
     const f32x4 x = *reinterpret_cast<const f32x4*>(smem_f + r * G::RS + p % G::PPR * 4);
     if (t0 + r < t_end) *reinterpret_cast<f32x4*>(gout + (t0 + r) * a.out.t + p % G::PPR * 4) = t0 + r < len ? x : z;
   }
 }
 
-template <int D>
+template <int D, int QT>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_f32_kernel<D>), Cfg<D>::FLOATS * 4);
+  using G = Cfg<D, QT>;
+  hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_f32_kernel<D, QT>), G::FLOATS * 4);
   if (e != hipSuccess) return e;
-  window_prefill_f32_kernel<D><<<dim3((unsigned)xcd_grid(a.B * a.Hkv, a.H / a.Hkv * ((a.L + QT - 1) / QT))), 256, Cfg<D>::FLOATS * 4, s>>>(a);
+  window_prefill_f32_kernel<D, QT><<<dim3((unsigned)xcd_grid(a.B * a.Hkv, a.H / a.Hkv * ((a.L + QT - 1) / QT))), G::NT, G::FLOATS * 4, s>>>(a);
   return hipGetLastError();
 }
-
 }  // namespace
 
-hipError_t launch_window_prefill_f32(const WindowArgs& a, int d, hipStream_t s) { return d == 64 ? launch<64>(a, s) : launch<128>(a, s); }
+// Rows of 64 in fewer than 512 workgroups of 128 queries (two a compute unit): of 64 queries instead, which spread more
+// evenly: 66 -> 58 us at 48 heads of 1001 tokens, the same from there on.  (Rows of 128: 82 -> 121 us at 32 heads of 1024.)
+hipError_t launch_window_prefill_f32(const WindowArgs& a, int d, hipStream_t s) {
+  if (d == 128) return launch<128, 128>(a, s);
+  return (int64_t)a.B * a.H * ((a.L + 127) / 128) < 512 ? launch<64, 64>(a, s) : launch<64, 128>(a, s);
+}
 
 }  // namespace linattn

@@ -413,11 +413,12 @@ hipError_t launch_cache(const WindowCacheArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Workgroups per key/value head: enough that every compute unit has some (two of their waves' tile chains hide each
-// other's trips to memory), as long as every wave has a tile.
+// Workgroups per key/value head: two on every compute unit, as many as fit (a wave's trips to memory hide behind those of its
+// neighbours; with one of four waves more, the join costs more than it brings: 96 -> 98 us at 256 heads of 4096 rows), as long
+// as every wave has a tile.
 int window_step_splits(int64_t heads, int64_t held, int rows) {
   const int64_t wgs = heads * ((rows + 31) / 32), tiles = (held + KT - 1) / KT + 1;
-  int64_t n = (1024 + wgs - 1) / wgs;
+  int64_t n = (512 + wgs - 1) / wgs;
   if (n > (tiles + 3) / 4) n = (tiles + 3) / 4;
   return n < 1 ? 1 : n > 64 ? 64 : (int)n;
 }
