@@ -87,7 +87,8 @@ linattn_status run(DecayArgs& a, const linattn_decay_desc* d, const Plan& p, voi
   hipError_t e = hipSuccess;
   if (p.nseg > 1) {
     e = bf16 ? launch_decay_first_pass_bf16(a, d->d, s) : launch_decay_first_pass_f32(a, d->d, s);
-    a.fold = p.nseg <= kFold;
+    // (in place: the last segment writes the state that the others would read)
+    a.fold = p.nseg <= kFold && !(a.S_in && a.S_in == a.S_out);
     if (e == hipSuccess && !a.fold) {
       const int dd = d->d * d->d;
       decay_scan_kernel<<<dim3(a.roles * a.B * a.H * (dd / 256)), 256, 0, s>>>(a, dd);

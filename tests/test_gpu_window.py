@@ -40,7 +40,8 @@ SHAPES = [  # B, H, Hkv, L, d, W, sinks, ragged
     (1, 1, 1, 1, 64, 1, 0, False), (2, 2, 1, 1, 128, 5, 3, False), (1, 2, 2, 31, 128, 7, 0, False), (1, 3, 1, 64, 64, 64, 1, False),
     (2, 4, 2, 65, 128, 1, 0, True), (1, 2, 1, 129, 64, 1, 64, False), (1, 2, 2, 300, 128, 33, 5, False), (4, 2, 1, 257, 64, 100, 4, True),
     (1, 8, 1, 517, 128, 128, 64, False), (1, 2, 1, 700, 64, 65, 33, False), (2, 2, 2, 400, 128, 100000, 2, True), (1, 1, 1, 1030, 64, 64, 0, False),
-    (2, 4, 2, 900, 128, 127, 1, True), (1, 1, 1, 130, 128, 2 ** 31 - 1, 64, False)]
+    (2, 4, 2, 900, 128, 127, 1, True), (1, 1, 1, 130, 128, 2 ** 31 - 1, 64, False),
+    (9, 16, 8, 70, 64, 20, 3, True), (4, 4, 2, 200, 64, 50, 3, True)]          # key/value heads dealt out whole over the chiplets
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
