@@ -335,25 +335,28 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
   }
 }
 
-// Gradient rows of k or v from their `slots` shares [bk][slot][2][n_rows][D].  SINKS: a sink's row a workgroup, its shares
-// dealt out over the threads; else several rows, all but the sinks' if these have shares of their own.
-template <int D, bool SINKS>
+// Gradient rows of k or v from their shares [bk][slot][2][n_rows][D].  The first workgroups of a head take a sink's row each, its
+// shares dealt out over the threads (they have the longest way); the others several of the other rows.
+template <int D>
 __global__ __launch_bounds__(256) void window_shares_kernel(WindowArgs a) {
   constexpr int LR = D / 4, PER = 256 / LR;      // threads of a row; rows (or slots) at a time
   __shared__ __attribute__((aligned(16))) float sum[PER][D];
   const int kv = blockIdx.x & 1, bk = blockIdx.x >> 1, b = bk / a.Hkv, hk = bk % a.Hkv;
   const int e = threadIdx.x % LR * 4, u = threadIdx.x / LR;
-  const int n_rows = SINKS ? a.sinks : a.L, slots = SINKS ? a.parts + 2 * a.far : a.parts;
-  const int row = SINKS ? blockIdx.y : blockIdx.y * PER + u;
+  const int n_sinks = a.far > 0 ? a.sinks : 0;
+  const bool sink = (int)blockIdx.y < n_sinks;
+  const int n_rows = sink ? a.sinks : a.L, slots = sink ? a.parts + 2 * a.far : a.parts;
+  const int row = sink ? blockIdx.y : (blockIdx.y - n_sinks) * PER + u;
+  if (!sink && (row >= a.L || row < n_sinks)) return;
   const int len = clamp_len(a.lens, b, a.L);
-  if (!SINKS && (row >= a.L || (a.far > 0 && row < a.sinks))) return;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   if (row < len) {
-    const float* p = (SINKS ? a.sink_part : a.part) + (((int64_t)bk * slots * 2 + kv) * n_rows + row) * D + e;
+    const float* p = (sink ? a.sink_part : a.part) + (((int64_t)bk * slots * 2 + kv) * n_rows + row) * D + e;
+    const int first = sink ? u : 0, step = sink ? PER : 1;
 #pragma unroll 4
-    for (int i = SINKS ? u : 0; i < slots; i += SINKS ? PER : 1) x += *reinterpret_cast<const f32x4*>(p + (int64_t)i * 2 * n_rows * D);
+    for (int i = first; i < slots; i += step) x += *reinterpret_cast<const f32x4*>(p + (int64_t)i * 2 * n_rows * D);
   }
-  if (SINKS) {
+  if (sink) {
     *reinterpret_cast<f32x4*>(&sum[u][e]) = x;
     __syncthreads();
     if (u > 0) return;
@@ -377,13 +380,9 @@ hipError_t launch(const WindowArgs& a, hipStream_t s) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   window_dkv_kernel<D><<<dim3((unsigned)xcd_grid(heads, a.far + a.parts * tiles)), 256, Cfg<D>::DKV_BYTES, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.parts > 1) {
-    constexpr int PER = 1024 / D;
-    window_shares_kernel<D, false><<<dim3(2 * heads, (a.L + PER - 1) / PER), 256, 0, s>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.far > 0) {
-    window_shares_kernel<D, true><<<dim3(2 * heads, a.sinks), 256, 0, s>>>(a);
+  const int n_sinks = a.far > 0 ? a.sinks : 0, blocks = n_sinks + (a.parts > 1 ? (a.L + 1024 / D - 1) / (1024 / D) : 0);
+  if (blocks > 0) {
+    window_shares_kernel<D><<<dim3(2 * heads, blocks), 256, 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;

@@ -92,8 +92,9 @@ def test_pointers():
 def test_workspace():
     lib = binding.load()
     need = lib.linattn_window_backward_workspace_bytes(ctypes.byref(desc()), 256)
-    assert need == 2 * 2 * 8 * 256 * 4 and backward(desc(), n=need - 1) == 6 and backward(desc(), ws=None) == 6
-    assert lib.linattn_window_backward_workspace_bytes(ctypes.byref(desc()), 1024) > 2 * 2 * 8 * 1024 * 4    # shares of the sinks' gradients
+    assert need >= 2 * (2 * 8 * 256) * 4 and backward(desc(), n=need - 1) == 6 and backward(desc(), ws=None) == 6
+    sizes = [lib.linattn_window_backward_workspace_bytes(ctypes.byref(desc(sinks=n)), 1024) for n in (0, 4, 64)]
+    assert sizes[0] < sizes[1] < sizes[2]                                   # shares of the sinks' gradients
     wide = desc(window=4096)
     need = lib.linattn_window_step_workspace_bytes(ctypes.byref(wide), 3)
     assert need > 0 and step(wide, kk=3, n=need - 1) == 6 and step(wide, kk=3, ws=None) == 6
