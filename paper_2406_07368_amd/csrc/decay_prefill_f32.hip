@@ -5,7 +5,8 @@
 // weight is converted or moved.  The 32 x 32 scores of a group are one tile; their contraction is cut over the waves
 // and the parts are added where they are read.
 //
-// Bound: the fp32 matrix rate (about 4 d^2 + 64 d flops a token and head against 16 d bytes).
+// Bound: the fp32 matrix rate (about 4 d^2 + 64 d flops a token and head against 16 d bytes).  Measured at 48 padded heads of 64 over
+// 1001 tokens, in 16 segments: 45 us, of which 28 this kernel.
 #include "common.h"
 #include "decay.h"
 #include "kernels.h"

@@ -15,7 +15,8 @@
 // query tiles that see nothing of it but sinks are shared out over workgroups of their own, and where there are few key
 // tiles each is shared by several workgroups.  Their sums (fp32) go to the workspace and are added up in a fixed order.
 //
-// Bound: the matrix cores (14 d flops a visible pair here).
+// Bound: LDS reads and vector ALUs beside the matrix cores (14 d flops a visible pair here).  Measured at 64 heads of 128 over sequences of
+// up to 4096 tokens, a window of 1024: dq 190 us, 810 TFLOP/s; dk and dv 336 us, 620 TFLOP/s.
 #include "common.h"
 #include "kernels.h"
 #include "mfma_util.h"
