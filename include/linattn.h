@@ -339,8 +339,9 @@ linattn_status linattn_decode(const linattn_desc *desc,
  *
  * Two operators for decoders whose layers keep a fixed amount of memory per sequence: linear attention with a decay for
  * each head (linattn_decay_*) and softmax attention over a sliding window with a few first tokens that stay visible
- * (linattn_window_*).  Each has a form for prompts, one for generation / verification steps, and a gradient.  The conventions at the top of this file hold, with these differences: the descriptors carry
- * strides for every tensor of rows, and `lens` gives every batch row a length of its own.
+ * (linattn_window_*).  Each has a form for prompts, one for generation / verification steps, and a gradient.  The
+ * conventions at the top of this file hold, with these differences: the descriptors carry strides for every tensor of
+ * rows, and `lens` gives every batch row a length of its own.
  *
  *   lens         in, optional  device int32 [B]: tokens of each batch row, clamped into 0..L; NULL = L for all.
  *                Rows behind a sequence's end are not read into anything (they may hold NaN); the output and gradient
@@ -375,7 +376,7 @@ typedef struct {
 size_t linattn_decay_workspace_bytes(const linattn_decay_desc *desc, int32_t L);
 size_t linattn_decay_backward_workspace_bytes(const linattn_decay_desc *desc, int32_t L);
 
-/* All L >= 0 tokens of every (b, h).
+/* All L tokens of every (b, h), 0 <= L <= 2^30.
  *   q, k, v      in   [B,H,L,d] by strides;  out  out  [B,H,L,d] by strides
  *   S_in         in, optional   float [B,H,d,d] dense (row = key feature), NULL = zeros
  *   S_out        out, optional  the state after lens[b] tokens; may be S_in
@@ -430,7 +431,7 @@ typedef struct {
 
 #define LINATTN_MAX_SINKS 64
 
-/* All L >= 0 tokens of every (b, h), from the start of the sequences.
+/* All L tokens of every (b, h), from the start of the sequences: 0 <= L <= 2^30, B * H * ceil(L / 128) <= 2^23.
  *   q [B,H,L,d], k, v [B,H_kv,L,d], out [B,H,L,d]  by strides
  *   lse          out, optional  float [B,H,L] dense; -inf behind a sequence's end
  *   kcache, vcache  out, optional (all three or none)  [B,H_kv,sinks+window,d] dense, i/o dtype: the rows that later

@@ -69,7 +69,7 @@ linattn_status check(const linattn_decay_desc* d, int32_t L, bool gradient, bool
   if (d->io_dtype != LINATTN_F32 && d->io_dtype != LINATTN_BF16) return LINATTN_ERR_DTYPE;
   if (d->B < 1 || d->H < 1 || (int64_t)d->B * d->H > (int64_t)1 << 20) return LINATTN_ERR_SHAPE;
   if (d->d != 64 && d->d != 128) return LINATTN_ERR_SHAPE;
-  if (!finite(d->scale) || d->reserved != 0 || L < 0) return LINATTN_ERR_SHAPE;
+  if (!finite(d->scale) || d->reserved != 0 || L < 0 || L > kMaxTokens) return LINATTN_ERR_SHAPE;
   if (!strides) return LINATTN_OK;
   bool ok = good_input(d->q, d->B, d->H, L) && good_input(d->k, d->B, d->H, L) && good_input(d->v, d->B, d->H, L);
   if (gradient)

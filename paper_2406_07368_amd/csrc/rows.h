@@ -7,6 +7,8 @@
 
 namespace linattn {
 
+constexpr int32_t kMaxTokens = 1 << 30;           // tile borders beyond the last token still fit 32 bits
+
 inline bool finite(float x) { return x - x == 0.f; }
 
 inline bool aligned16_all(std::initializer_list<const void*> ptrs) {

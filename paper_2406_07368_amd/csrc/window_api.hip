@@ -11,8 +11,6 @@ using namespace linattn;
 
 namespace {
 
-constexpr int32_t kMaxL = 1 << 30;                // tile borders beyond the last token still fit 32 bits
-
 linattn_status check(const linattn_window_desc* d, int32_t L) {
   if (!d) return LINATTN_ERR_NULL;
   if (d->io_dtype != LINATTN_F32 && d->io_dtype != LINATTN_BF16) return LINATTN_ERR_DTYPE;
@@ -20,7 +18,7 @@ linattn_status check(const linattn_window_desc* d, int32_t L) {
   if (d->d != 64 && d->d != 128) return LINATTN_ERR_SHAPE;
   if (d->window < 1 || d->sinks < 0 || d->sinks > LINATTN_MAX_SINKS) return LINATTN_ERR_SHAPE;
   if (!finite(d->scale) || d->scale < 0.f) return LINATTN_ERR_SHAPE;
-  if (L < 0 || L > kMaxL || (int64_t)d->B * d->H * ((L + 127) / 128) > (int64_t)1 << 23) return LINATTN_ERR_SHAPE;   // (a grid's limit)
+  if (L < 0 || L > kMaxTokens || (int64_t)d->B * d->H * ((L + 127) / 128) > (int64_t)1 << 23) return LINATTN_ERR_SHAPE;   // (a grid's limit)
   return LINATTN_OK;
 }
 linattn_status check_rows(const linattn_window_desc* d, int32_t L, bool gradient) {

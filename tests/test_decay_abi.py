@@ -71,6 +71,16 @@ def test_sizes():
         assert step(desc(), kk=kk) == 2
 
 
+def test_more_tokens_than_fit():
+    huge = dict(q=(0, 0, 0), k=(0, 0, 0), v=(0, 0, 0), dout=(0, 0, 0), B=1, H=1)
+    lib = binding.load()
+    for L in ((1 << 30) + 1, (1 << 31) - 1):      # (walks of 64 tokens would pass 32 bits)
+        assert prefill(desc(**huge), L=L) == 2 and backward(desc(**huge), L=L) == 2
+        for f in (lib.linattn_decay_workspace_bytes, lib.linattn_decay_backward_workspace_bytes):
+            assert f(ctypes.byref(desc(**huge)), L) == 0
+    assert lib.linattn_decay_workspace_bytes(ctypes.byref(desc(**huge)), 1 << 30) > 0
+
+
 def test_pointers():
     for call, names in ((prefill, ("q", "k", "v", "log_decay", "out")), (backward, ("q", "k", "v", "log_decay", "dout", "dq", "dk", "dv")),
                         (step, ("q", "k", "v", "log_decay", "S", "out"))):
