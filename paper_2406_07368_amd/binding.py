@@ -215,10 +215,18 @@ def make_decay_desc(B, H, d, io_dtype=torch.bfloat16, scale=1.0, **strides) -> D
     return DecayDesc(B, H, d, code, float(scale), 0, **{n: Strides(*[int(x) for x in s]) for n, s in strides.items()})
 
 
+def _int32(name, x) -> int:
+    """A field of 32 bits: ctypes would cut off what is above them."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} must fit 32 bits")
+    return x
+
+
 def make_window_desc(B, H, H_kv, d, window, sinks=0, io_dtype=torch.bfloat16, scale=1.0, **strides) -> WindowDesc:
     """strides: as for ``make_decay_desc``."""
     code = {torch.float32: LINATTN_F32, torch.bfloat16: LINATTN_BF16}[io_dtype]
-    return WindowDesc(B, H, H_kv, d, code, int(window), int(sinks), float(scale), **{n: Strides(*[int(x) for x in s]) for n, s in strides.items()})
+    return WindowDesc(B, H, H_kv, d, code, _int32("window", window), _int32("sinks", sinks), float(scale), **{n: Strides(*[int(x) for x in s]) for n, s in strides.items()})
 
 
 def linattn_set_wait_limit(spins: int) -> int:
@@ -540,11 +548,11 @@ def _on(device):
 def decay_prefill(q, k, v, log_decay, scale=None, state=None, lens=None, want_state=True, stream=None):
     """Linear attention with a decay for each head: out_t = scale * q_t^T S_t, S_t = exp(log_decay) S_{t-1} + k_t v_t^T.
 
-    q, k, v: [B,H,L,d] CUDA tensors, fp32 or bf16, of any strides that are contiguous along d (slices of a packed
-    projection, token-major views, broadcast heads).  log_decay: fp32 [H], each <= 0.  scale: None for d ** -0.5.
-    state: None or the fp32 [B,H,d,d] to go on from.  lens: None, or int32 [B], the tokens of each row; rows behind
-    them are ignored and their outputs are zeros.  Returns out (q's layout where q is dense in some order of its axes)
-    and the new state (None if not wanted)."""
+    q, k, v: [B,H,L,d] CUDA tensors, fp32 or bf16, contiguous along d and otherwise of any strides that are multiples of 8
+    (slices of a packed projection, token-major views, broadcast heads), at multiples of 16 bytes.  log_decay: fp32 [H],
+    each <= 0.  scale: None for d ** -0.5.  state: None or the fp32 [B,H,d,d] to go on from.  lens: None, or int32 [B],
+    the tokens of each row; rows behind them are ignored and their outputs are zeros.  Returns out (q's layout where q is
+    dense in some order of its axes) and the new state (None if not wanted)."""
     if stream is None:
         r = _native().decay_prefill(q, k, v, log_decay, scale, state, lens, want_state)
         if r is not None:
@@ -566,8 +574,8 @@ def decay_prefill(q, k, v, log_decay, scale=None, state=None, lens=None, want_st
 
 
 def decay_backward(q, k, v, log_decay, dout, scale=None, lens=None, stream=None):
-    """Gradient of ``decay_prefill`` (from no state) with respect to q, k and v; dout: [B,H,L,d], any strides that are
-    contiguous along d.  Returns dq, dk, dv."""
+    """Gradient of ``decay_prefill`` (from no state) with respect to q, k and v; dout: [B,H,L,d], strides as
+    there.  Returns dq, dk, dv."""
     if stream is None:
         r = _native().decay_backward(q, k, v, log_decay, dout, scale, lens)
         if r is not None:
@@ -608,8 +616,9 @@ def decay_step(q, k, v, log_decay, state, scale=None, n_commit=None, stream=None
     return out
 
 
-def _kv(where, q, k, v):
-    """Key/value rows [B,H_kv,L,d] for queries [B,H,L,d]."""
+def _kv(where, q, k, v, window, sinks):
+    """Key/value rows [B,H_kv,L,d] for queries [B,H,L,d]; the numbers."""
+    _int32(f"{where}: window", window), _int32(f"{where}: sinks", sinks)
     if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.shape[1] < 1 or q.shape[1] % k.shape[1]:
         raise ValueError(f"{where}: k and v must have one shape, q's with a number of heads that divides q's")
 
@@ -623,9 +632,8 @@ def window_cache(B, H_kv, d, window, sinks=0, dtype=torch.bfloat16, device="cuda
 def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=False, want_cache=False, stream=None):
     """Softmax attention in which token t sees token s where s <= t and (s > t - window or s < sinks).
 
-    q: [B,H,L,d], k, v: [B,H_kv,L,d] (H_kv divides H: query head h uses key/value head h // (H // H_kv)), fp32 or bf16, of
-    any strides that are contiguous along d.  scale: None for d ** -0.5.  lens: None, or int32 [B], the tokens of each
-    row; rows behind them are ignored and their outputs are zeros.  sinks: at most 64.  Returns out, the logarithms of the
+    q: [B,H,L,d], k, v: [B,H_kv,L,d] (H_kv divides H: query head h uses key/value head h // (H // H_kv)), fp32 or bf16,
+    strides as for ``decay_prefill``.  scale: None for d ** -0.5.  lens: None, or int32 [B], the tokens of each row; rows behind them are ignored and their outputs are zeros.  sinks: at most 64.  Returns out, the logarithms of the
     softmax sums (fp32 [B,H,L], what ``window_backward`` takes; None if not wanted) and the cache for ``window_step``
     (kcache, vcache, pos; None if not wanted)."""
     if stream is None and not want_cache:
@@ -633,7 +641,7 @@ def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=Fal
         if r is not None:
             return _result(r, "linattn_window_prefill")
     _rows("window_prefill", q, k=k, v=v)
-    _kv("window_prefill", q, k, v)
+    _kv("window_prefill", q, k, v, window, sinks)
     B, H, L, d = q.shape
     _aux("window_prefill", "lens", lens, torch.int32, (B,), q.device)
     with _on(q.device):
@@ -653,7 +661,7 @@ def window_backward(q, k, v, out, lse, dout, window, sinks=0, scale=None, lens=N
         if r is not None:
             return _result(r, "linattn_window_backward")
     _rows("window_backward", q, k=k, v=v, out=out, dout=dout)
-    _kv("window_backward", q, k, v)
+    _kv("window_backward", q, k, v, window, sinks)
     B, H, L, d = q.shape
     if out.shape != q.shape or dout.shape != q.shape:
         raise ValueError("window_backward: out and dout must have q's shape")
@@ -679,7 +687,7 @@ def window_step(q, k, v, cache, window, sinks=0, scale=None, n_commit=None, stre
         if r is not None:
             return _result(r, "linattn_window_step")
     _rows("window_step", q, k=k, v=v)
-    _kv("window_step", q, k, v)
+    _kv("window_step", q, k, v, window, sinks)
     B, H, kk, d = q.shape
     kcache, vcache, pos = cache
     for n, x in (("q", q), ("k", k), ("v", v)):

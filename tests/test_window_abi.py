@@ -106,6 +106,16 @@ def test_no_tokens_is_no_work():
     assert backward(desc(), L=0, q=None, k=None, v=None, out=None, lse=None, dout=None, dq=None, dk=None, dv=None) == 0
 
 
+def test_numbers_of_more_than_32_bits_are_not_cut():
+    q = torch.zeros(1, 1, 4, 64)
+    for kw in (dict(window=(1 << 32) + 5), dict(window=5, sinks=1 << 32), dict(window=-(1 << 32) + 5)):
+        for call, more in ((binding.window_prefill, {}), (binding.window_backward, dict(out=q, lse=torch.zeros(1, 1, 4), dout=q))):
+            with pytest.raises(ValueError, match="32 bits"):
+                call(q=q, k=q, v=q, **more, **kw)
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.make_window_desc(1, 1, 1, 64, **kw)
+
+
 def test_tensor_level_calls_refuse():
     q, k, f = torch.zeros(2, 4, 8, 64), torch.zeros(2, 2, 8, 64), torch.zeros(2, 4, 8)
     cache = binding.window_cache(2, 2, 64, 10, 3, torch.float32, "cpu")
