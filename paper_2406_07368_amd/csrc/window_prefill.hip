@@ -3,15 +3,15 @@
 //   out_t = sum_s p_ts v_s / sum_s p_ts,   p_ts = exp(scale q_t.k_s - m_t),   s <= t and (s > t - window or s < sinks)
 //
 // One pass over the visible keys with a running maximum m and a running sum.  A workgroup takes 128 queries of a head,
-// a wave 32 of them; 64 keys at a time lie in one of two LDS buffers while the next 64 are on their way in registers.
+// a wave 32 of them; 64 or 32 keys at a time lie in one of two LDS buffers while the next are on their way into the other.
 // S^T = K Q^T with the keys in the accumulator's rows and a query per lane, so a query's statistics are a lane's own
 // (and its partner's 32 lanes on), and the weights, packed to bf16, are the operand of O^T += V^T P^T as they stand: the
 // accumulator layout is the operand layout up to a permutation of the keys, which is applied to the transposed reads of
 // V.  Key tiles that no query of the tile sees are not visited; masks are computed only where a border crosses.
 //
-// Bound: the vector ALUs (some 190 instructions for 32 products of a wave, 32 of them exponentials) beside the matrix cores (4 d flops a
-// visible pair), at 1.95 GHz (power).  Measured at 64 heads of 128 over 8192 tokens, a window of 2048: 530 us, 910 TFLOP/s of 1361 that a
-// large library product reaches.
+// Bound: the vector ALUs (some 190 instructions for 32 products of a wave, 32 of them exponentials; 55 % of the cycles) beside the matrix
+// cores (4 d flops a visible pair; 52 %), at 1.8 GHz (power).  Measured at 64 heads of 128 over 8192 tokens, a window of 2048: 505 to 525 us
+// (boards differ), 940 TFLOP/s of 1361 that a large library product reaches.
 #include "common.h"
 #include "kernels.h"
 #include "mfma_util.h"
@@ -21,11 +21,11 @@ namespace linattn {
 
 namespace {
 
-constexpr int QT = 128, KT = 64;
+constexpr int QT = 128;                         // queries of a workgroup; KT: keys at a time
 
 constexpr float kLate = 8.f;   // log2: how far a running maximum may lie behind before the sums are scaled anew
 
-template <int D>
+template <int D, int KT>
 struct Cfg {
   static constexpr int BUF = 2 * KT * D;        // elements: K, V
   static constexpr int OS = D + 8;              // finished rows
@@ -33,9 +33,9 @@ struct Cfg {
   static constexpr int PPR = D / 8;
 };
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
-  using G = Cfg<D>;
+template <int D, int KT>
+__global__ __launch_bounds__(256, KT == 32 ? 3 : 2) void window_prefill_kernel(WindowArgs a) {
+  using G = Cfg<D, KT>;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
   // the query heads that share keys side by side, then the query tiles
   const int group = a.H / a.Hkv, ntile = (a.L + QT - 1) / QT;
@@ -63,6 +63,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
   const uint16_t* gk = static_cast<const uint16_t*>(a.k.p) + b * a.k.b + hk * a.k.h;
   const uint16_t* gv = static_cast<const uint16_t*>(a.v.p) + b * a.v.b + hk * a.v.h;
   const float c = window_log2_scale(a.scale);
+  constexpr int KS = D / 16, CT = D / 32, NS = KT / 32 * KS, NP = KT / 16 * CT, AHEAD = KT == 32 ? 2 : D == 128 ? 6 : 3;
   const Swizzled<D> lds(lane, 4);
 
   const int t = t0 + 32 * w + l32;              // this lane's query
@@ -76,11 +77,11 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
   // key tiles: those of the sinks that lie before the window's, then the window's
   const int last = (t_end < len ? t_end : len) - 1;
   const int lo = (t0 - a.window + 1 > 0 ? t0 - a.window + 1 : 0) / KT;
-  const int ns = a.sinks > 0 && lo > 0 ? 1 : 0; // (64 sinks at most: one tile)
+  const int sink_tiles = (a.sinks + KT - 1) / KT, ns = sink_tiles < lo ? sink_tiles : lo;
   const int nk = ns + last / KT - lo + 1;
   auto key0 = [&](int i) { return (i < ns ? i : lo + i - ns) * KT; };
 
-  const Fetch<D> fetch(tid);
+  const Fetch<D, KT> fetch(tid);
   auto request = [&](int i, uint16_t* buf) {
     const int s0 = key0(i);
     fetch.request(buf, gk + s0 * a.k.t, a.k.t, len - s0);
@@ -103,23 +104,33 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
     const uint16_t* Vl = Kl + KT * D;
     const int s0 = key0(i);
     if (!(s0 <= tw + 31 && (s0 + KT - 1 > tw - a.window || s0 < a.sinks))) return;
-    f32x16 x[2] = {};
+    // the matrix operands in the order of their use, AHEAD of them read before they are needed
+    bf16x8 op[NS + NP];
+    auto read = [&](int i) {
+      if (i < NS) op[i] = lds.rows(Kl, 32 * (i / KS), i % KS);
+      else if (i < NS + NP) op[i] = lds.cols_acc(Vl, 16 * ((i - NS) / CT), (i - NS) % CT);
+    };
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int i = 0; i < AHEAD; ++i) read(i);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 x[KT / 32] = {};
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) x[kt] = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x[kt]);
-    read_ahead<6, 1, 1, D / 8>();
+    for (int i = 0; i < NS; ++i) {
+      x[i / KS] = mfma(op[i], qop[i % KS], x[i / KS]);
+      read(i + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     const bool all = s0 + KT - 1 <= tw && (s0 > tw + 31 - a.window || s0 + KT <= a.sinks);
     if (!all) {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < KT / 32; ++kt)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (!window_sees(t, s0 + 32 * kt + acc_row(r, hi), a.window, a.sinks)) x[kt][r] = -__builtin_inff();
     }
     float top = x[0][0];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < KT / 32; ++kt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[kt][r]);
     top = max_xor32(top) * c;
@@ -132,19 +143,27 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
       for (int ct = 0; ct < D / 32; ++ct) O[ct] *= f;
     }
     const float mm = m == -__builtin_inff() ? 0.f : m;         // nothing seen yet: every weight is exp2(-inf)
+    auto weigh = [&](int j, int from, int to) {                // 16 keys: eight of this lane
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-#pragma unroll
-        for (int r = 8 * half; r < 8 * half + 8; ++r) {
-          x[kt][r] = __builtin_amdgcn_exp2f(x[kt][r] * c - mm);
-          l += x[kt][r];
-        }
-        const bf16x8 p = pack8(x[kt], 8 * half);
-#pragma unroll
-        for (int ct = 0; ct < D / 32; ++ct) O[ct] = mfma(lds.cols_acc(Vl, 32 * kt + 16 * half, ct), p, O[ct]);
+      for (int r = from; r < to; ++r) {
+        const int i = 8 * (j % 2) + r;
+        x[j / 2][i] = __builtin_amdgcn_exp2f(x[j / 2][i] * c - mm);
+        l += x[j / 2][i];
       }
+    };
+    weigh(0, 0, 8);
+#pragma unroll
+    for (int j = 0; j < KT / 16; ++j) {
+      const bf16x8 p = pack8(x[j / 2], 8 * (j % 2));
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        __builtin_amdgcn_sched_barrier(0);
+        O[ct] = mfma(op[NS + CT * j + ct], p, O[ct]);
+        read(NS + CT * j + ct + AHEAD);
+        if (j + 1 < KT / 16) weigh(j + 1, 8 * ct / CT, 8 * (ct + 1) / CT);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   auto turn = [&](int i, uint16_t* __restrict cur, uint16_t* __restrict next) {   // (see Fetch)
     arrive(i, cur);
@@ -179,16 +198,22 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WindowArgs a) {
   }
 }
 
-template <int D>
-hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_kernel<D>), Cfg<D>::BYTES);
+template <int D, int KT>
+hipError_t launch(const WindowArgs& a, int64_t grid, hipStream_t s) {
+  hipError_t e = LINATTN_MAX_LDS_ONCE((window_prefill_kernel<D, KT>), (Cfg<D, KT>::BYTES));
   if (e != hipSuccess) return e;
-  window_prefill_kernel<D><<<dim3((unsigned)xcd_grid(a.B * a.Hkv, a.H / a.Hkv * ((a.L + QT - 1) / QT))), 256, Cfg<D>::BYTES, s>>>(a);
+  window_prefill_kernel<D, KT><<<dim3((unsigned)grid), 256, Cfg<D, KT>::BYTES, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_window_prefill_bf16(const WindowArgs& a, int d, hipStream_t s) { return d == 64 ? launch<64>(a, s) : launch<128>(a, s); }
+hipError_t launch_window_prefill_bf16(const WindowArgs& a, int d, hipStream_t s) {
+  const int64_t grid = xcd_grid(a.B * a.Hkv, a.H / a.Hkv * ((a.L + QT - 1) / QT));
+  if (d == 64) return launch<64, 64>(a, grid, s);
+  // 32 keys at a time leave room for three workgroups on a compute unit, where there are as many: 540 -> 524 us at the size above.
+  // Where there are fewer a wave is alone with what it waits for, twice as often: 151 -> 211 us at 4 heads over 8192 tokens.
+  return grid >= 3 * 256 ? launch<128, 32>(a, grid, s) : launch<128, 64>(a, grid, s);
+}
 
 }  // namespace linattn

@@ -58,6 +58,19 @@ def test_prefill(dtype, B, H, Hkv, L, d, W, sinks, ragged):
     assert torch.equal(out, binding.window_prefill(*cuda(q, k, v), W, sinks, 0.2, *cuda(lens))[0])
 
 
+@pytest.mark.parametrize("W,sinks", [(1, 0), (40, 33), (97, 64), (1000, 1)])
+def test_prefill_with_workgroups_for_the_whole_chip(W, sinks):
+    """Fewer keys at a time, so that more workgroups fit a compute unit."""
+    B, H, Hkv, L, d = 16, 16, 4, 301, 128
+    q, = rows(B, H, L, d, BF, 21)
+    k, v = rows(B, Hkv, L, d, BF, 22, 2)
+    lens = some_lens(B, L)
+    want, wl, size = plain(q.double(), k.double(), v.double(), W, sinks, 0.2, lens)
+    out, lse, _ = binding.window_prefill(*cuda(q, k, v), W, sinks, 0.2, *cuda(lens), want_lse=True)
+    near(out, want, size, BF, ROUNDINGS[BF], "out", NORM[BF])
+    check_lse(lse, wl)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_scores_far_apart_and_equal(dtype):
     """Weights that underflow next to one that does not, a maximum that moves with every tile, and a scale of 0."""
