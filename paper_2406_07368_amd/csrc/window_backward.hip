@@ -16,7 +16,7 @@
 // tiles each is shared by several workgroups.  Their sums (fp32) go to the workspace and are added up in a fixed order.
 //
 // Bound: LDS reads and vector ALUs beside the matrix cores (14 d flops a visible pair here).  Measured at 64 heads of 128 over sequences of
-// up to 4096 tokens, a window of 1024: dq 190 us, 810 TFLOP/s; dk and dv 336 us, 620 TFLOP/s.
+// up to 4096 tokens, a window of 1024: dq 183 us, 840 TFLOP/s; dk and dv 321 us, 650 TFLOP/s.
 #include "common.h"
 #include "kernels.h"
 #include "mfma_util.h"
@@ -127,6 +127,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
     fetch.trim(buf + 64 * D, n, tid);
     __syncthreads();
   };
+  constexpr int AHEAD = 3;
   f32x16 dQ[G::CT];
 #pragma unroll
   for (int i = 0; i < G::CT; ++i) dQ[i] = f32x16{};
@@ -136,26 +137,50 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
     for (int kt = 0; kt < 2; ++kt) {
       const int sw = key0(i) + 32 * kt;
       if (!(sw <= tw + 31 && (sw + 31 > tw - a.window || sw < a.sinks))) continue;
+      // the matrix operands in the order of their use, AHEAD of each kind read before they are needed
+      bf16x8 ko[G::KS], vo[G::KS], kt_op[2 * G::CT];
+      auto read = [&](int j) {
+        if (j < G::KS) {
+          ko[j] = lds.rows(Kl, 32 * kt, j);
+          vo[j] = lds.rows(Vl, 32 * kt, j);
+        } else if (j < G::KS + 2 * G::CT) {
+          const int n = j - G::KS;
+          kt_op[n] = lds.cols_acc(Kl, 32 * kt + 16 * (n / G::CT), n % G::CT);
+        }
+      };
       f32x16 x = {}, y = {};
 #pragma unroll
+      for (int j = 0; j < AHEAD; ++j) read(j);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
       for (int ks = 0; ks < G::KS; ++ks) {
-        x = mfma(lds.rows(Kl, 32 * kt, ks), qop[ks], x);
-        y = mfma(lds.rows(Vl, 32 * kt, ks), dop[ks], y);
+        x = mfma(ko[ks], qop[ks], x);
+        y = mfma(vo[ks], dop[ks], y);
+        read(ks + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      read_ahead<6, 1, 1, 2 * G::KS>();
       const bool all = sw + 31 <= tw && (sw > tw + 31 - a.window || sw + 32 <= a.sinks);
+      auto weigh = [&](int from, int to) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r] * c - lse2) * (y[r] - delta);
-      if (!all) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!window_sees(t, sw + acc_row(r, hi), a.window, a.sinks)) x[r] = 0.f;
-      }
+        for (int r = from; r < to; ++r) x[r] = __builtin_amdgcn_exp2f(x[r] * c - lse2) * (y[r] - delta);
+      };
+      weigh(0, 8);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
+        if (!all) {
+#pragma unroll
+          for (int r = 8 * half; r < 8 * half + 8; ++r)
+            if (!window_sees(t, sw + acc_row(r, hi), a.window, a.sinks)) x[r] = 0.f;
+        }
         const bf16x8 p = pack8(x, 8 * half);
 #pragma unroll
-        for (int ct = 0; ct < G::CT; ++ct) dQ[ct] = mfma(lds.cols_acc(Kl, 32 * kt + 16 * half, ct), p, dQ[ct]);
+        for (int ct = 0; ct < G::CT; ++ct) {
+          __builtin_amdgcn_sched_barrier(0);
+          dQ[ct] = mfma(kt_op[G::CT * half + ct], p, dQ[ct]);
+          read(G::KS + G::CT * half + ct + AHEAD);
+          if (half == 0) weigh(8 + 8 * ct / G::CT, 8 + 8 * (ct + 1) / G::CT);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
@@ -229,12 +254,20 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
   const int q_lo = sink_job ? end : s0 / kWindowQ;
   const int q_n = (sink_job ? q_len : end) - q_lo > 0 ? (sink_job ? q_len : end) - q_lo : 0;
   const int step = sink_job ? a.far : a.parts;
-  const int items = q_n * group;
+  // an item, in base q_n as it were, and the one a step on
+  struct Item { int head, tile; };
+  const int step_head = q_n > 0 ? step / q_n : 0, step_tile = q_n > 0 ? step % q_n : 0;
+  auto after = [&](Item it) {
+    it.head += step_head;
+    it.tile += step_tile;
+    if (it.tile >= q_n) { it.tile -= q_n; ++it.head; }
+    return it;
+  };
 
   const Fetch<D, kWindowQ> fetch(tid);
-  auto first_row = [&](int it) { return (q_lo + it % q_n) * kWindowQ; };
-  auto request = [&](int it, uint16_t* buf, float* st) {
-    const int h = hk * group + it / q_n, t0 = first_row(it), n = len - t0;
+  auto first_row = [&](Item it) { return (q_lo + it.tile) * kWindowQ; };
+  auto request = [&](Item it, uint16_t* buf, float* st) {
+    const int h = hk * group + it.head, t0 = first_row(it), n = len - t0;
     fetch.request(buf, static_cast<const uint16_t*>(a.q.p) + b * a.q.b + h * a.q.h + t0 * a.q.t, a.q.t, n);
     fetch.request(buf + kWindowQ * D, static_cast<const uint16_t*>(a.dout.p) + b * a.dout.b + h * a.dout.h + t0 * a.dout.t, a.dout.t, n);
     if (w == 0) {                                // lanes: lse in base 2, then delta (behind the end: the last token's)
@@ -243,7 +276,7 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
       __builtin_amdgcn_global_load_lds((typename Fetch<D>::global_ptr)from, (typename Fetch<D>::lds_ptr)st, 4, 0, 0);
     }
   };
-  auto arrive = [&](int it, uint16_t* buf) {
+  auto arrive = [&](Item it, uint16_t* buf) {
     const int n = len - first_row(it);
     fetch.arrived();
     fetch.trim(buf, n, tid);
@@ -254,23 +287,42 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
   f32x16 dK[G::CT], dV[G::CT];
 #pragma unroll
   for (int i = 0; i < G::CT; ++i) { dK[i] = f32x16{}; dV[i] = f32x16{}; }
-  auto tile_of = [&](int it, int turn, const uint16_t* Ql, const float* st) {
+  auto tile_of = [&](Item it, int turn, const uint16_t* Ql, const float* st) {
     const uint16_t* dl = Ql + kWindowQ * D;
     const int tw = first_row(it);
     if (sink_job ? (turn & 1) != w >> 1 || kw >= a.sinks : !(kw <= tw + 31 && (kw + 31 > tw - a.window || kw < a.sinks))) return;
-    f32x16 x = {}, y = {};
     int vo = (kw - s0) * D;
     Swizzled<D> at = lds;                        // (addresses kept over the loop would not fit the registers)
     asm volatile("" : "+s"(vo));
-    at.forget_rows();
+    at.forget_rows(); at.forget_cols();
+    // the matrix operands in the order of their use, AHEAD of each kind read before they are needed (two: spills, which wait for the rows
+    // under way, 613 -> 650 us)
+    bf16x8 qo[G::KS], od[G::KS], vv[G::KS], dt[2 * G::CT], qt[2 * G::CT];
+    auto read = [&](int i) {
+      if (i < G::KS) {
+        qo[i] = at.rows(Ql, 0, i);
+        od[i] = at.rows(dl, 0, i);
+        vv[i] = at.rows(Vl + vo, 0, i);
+      } else if (i < G::KS + 2 * G::CT) {
+        const int j = i - G::KS;
+        dt[j] = at.cols_acc(dl, 16 * (j / G::CT), j % G::CT);
+        qt[j] = at.cols_acc(Ql, 16 * (j / G::CT), j % G::CT);
+      }
+    };
+    constexpr int AHEAD = 1;
+    f32x16 x = {}, y = {};
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read(i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int ks = 0; ks < G::KS; ++ks) {
-      x = mfma(at.rows(Ql, 0, ks), kop[ks], x);
-      y = mfma(at.rows(dl, 0, ks), at.rows(Vl + vo, 0, ks), y);
+      x = mfma(qo[ks], kop[ks], x);
+      y = mfma(od[ks], vv[ks], y);
+      read(ks + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (D == 128) read_ahead<9, 3, 2, 16>();
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
+    const bool all = kw + 31 <= tw && (kw > tw + 31 - a.window || kw + 32 <= a.sinks) && tw + 32 <= len;
+    auto weigh = [&](int r4) {
       const f32x4 le = *reinterpret_cast<const f32x4*>(st + 8 * r4 + 4 * hi);
       const f32x4 de = *reinterpret_cast<const f32x4*>(st + kWindowQ + 8 * r4 + 4 * hi);
 #pragma unroll
@@ -278,40 +330,48 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
         x[4 * r4 + i] = __builtin_amdgcn_exp2f(x[4 * r4 + i] * c - le[i]);
         y[4 * r4 + i] = x[4 * r4 + i] * (y[4 * r4 + i] - de[i]);
       }
-    }
-    const bool all = kw + 31 <= tw && (kw > tw + 31 - a.window || kw + 32 <= a.sinks) && tw + 32 <= len;
-    if (!all) {
+    };
+    auto mask = [&](int half) {
+      if (!all) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int t = tw + acc_row(r, hi);
-        if (!(window_sees(t, s, a.window, a.sinks) && t < len)) { x[r] = 0.f; y[r] = 0.f; }
+        for (int r = 8 * half; r < 8 * half + 8; ++r) {
+          const int t = tw + acc_row(r, hi);
+          if (!(window_sees(t, s, a.window, a.sinks) && t < len)) { x[r] = 0.f; y[r] = 0.f; }
+        }
       }
-    }
-    at.forget_cols();
+    };
+    weigh(0); weigh(1);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
+      mask(half);
       const bf16x8 p = pack8(x, 8 * half), ds = pack8(y, 8 * half);
 #pragma unroll
       for (int ct = 0; ct < G::CT; ++ct) {
-        dV[ct] = mfma(at.cols_acc(dl, 16 * half, ct), p, dV[ct]);
-        dK[ct] = mfma(at.cols_acc(Ql, 16 * half, ct), ds, dK[ct]);
+        __builtin_amdgcn_sched_barrier(0);
+        dV[ct] = mfma(dt[G::CT * half + ct], p, dV[ct]);
+        dK[ct] = mfma(qt[G::CT * half + ct], ds, dK[ct]);
+        read(G::KS + G::CT * half + ct + AHEAD);
+        if (half == 0 && ct < 2) weigh(2 + ct);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (D == 128) read_ahead<4, 2, 1, 16>();
   };
   uint16_t *even = smem + 128 * D, *odd = even + 2 * kWindowQ * D;
-  if (part < items) request(part, even, stats);
+  Item it = q_n > 0 ? Item{part / q_n, part % q_n} : Item{group, 0};
+  if (it.head < group) request(it, even, stats);
   vfetch.arrived();
 #pragma unroll
   for (int i = 0; i < 2; ++i) vfetch.trim(Vl + i * 64 * D, len - s0 - 64 * i, tid);
-  auto one = [&](int it, int turn, uint16_t* __restrict cur, float* __restrict st, uint16_t* __restrict next, float* __restrict st_next) {
+  auto one = [&](Item it, Item next_it, int turn, uint16_t* __restrict cur, float* __restrict st, uint16_t* __restrict next, float* __restrict st_next) {
     arrive(it, cur);
-    if (it + step < items) request(it + step, next, st_next);
+    if (next_it.head < group) request(next_it, next, st_next);
     tile_of(it, turn, cur, st);
   };
-  for (int it = part, turn = 0; it < items; it += 2 * step, turn += 2) {
-    one(it, turn, even, stats, odd, stats + 2 * kWindowQ);
-    if (it + step < items) one(it + step, turn + 1, odd, stats + 2 * kWindowQ, even, stats);
+  for (int turn = 0; it.head < group; turn += 2) {
+    const Item second = after(it);
+    one(it, second, turn, even, stats, odd, stats + 2 * kWindowQ);
+    it = after(second);
+    if (second.head < group) one(second, it, turn + 1, odd, stats + 2 * kWindowQ, even, stats);
   }
   if (!sink_job && a.parts == 1) {
     store_tile<D>(smem, dK, a.scale, gdk, a.dk.t, s0, s_end, len, tid);
