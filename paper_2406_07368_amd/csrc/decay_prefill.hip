@@ -16,14 +16,14 @@
 // the other is worked on (swizzle.h); finished rows leave through LDS, so that whole rows are stored.
 // V' enters the state as the sum of TERMS bf16 terms.  Two carry sixteen significant bits: with one, the gradient's error was
 // 1.65 times that of the final rounding alone, with two it is 1.4 times.  A state that is handed back in fp32 takes three, all
-// of an fp32 product's bits (its error at LLaMA size: 3.6e-7, with two terms 2.5e-6, for 275 us in the place of 256).
+// of an fp32 product's bits (its error at LLaMA size: 3.6e-7, with two terms 2.5e-6, for 264 us in the place of 240).
 //
 // The gradient is the same function with other roles: dq = F(dout, v, k), and over reversed time dk = F(v, dout, q),
 // dv = F(k, q, dout); a launch carries up to three roles.
 //
 // HBM is the floor (8 d bytes a token and head: at d = 128 1 KB, against 82 K flops), and what bounds it now is the issue of vector
-// and matrix instructions at the clock that the power limit leaves (2.0 GHz).  Measured at 256 heads of 128 over 4096 tokens: 248 us with
-// two terms, 278 with three (1.07 GB of rows: 4.4 and 3.9 TB/s; a copy runs at 5.1).
+// and matrix instructions at the clock that the power limit leaves (2.0 GHz).  Measured at 256 heads of 128 over 4096 tokens: 240 us with
+// two terms, 264 with three (1.07 GB of rows: 4.5 and 4.1 TB/s; a copy runs at 5.1).
 #include "common.h"
 #include "decay.h"
 #include "kernels.h"
@@ -196,11 +196,16 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
       for (int i = 0; i < G::TW; ++i) {
         const int nt = w + i * G::NW, tb = tile_row(nt), sb = nt - tb * (tb + 1) / 2;
         if (nt < 10) {
+          bf16x8 ko[D / 32], qo[D / 32];
+#pragma unroll
+          for (int ks = 0; ks < D / 32; ++ks) {
+            ko[ks] = lds_row8(Kl + 16 * sb * D + (t16 ^ (ks << 3)));
+            qo[ks] = lds_row8(Ql + 16 * tb * D + (t16 ^ (ks << 3)));
+          }
+          __builtin_amdgcn_sched_barrier(0);
           f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ks = 0; ks < D / 32; ++ks)
-            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row8(Kl + 16 * sb * D + (t16 ^ (ks << 3))),
-                                                        lds_row8(Ql + 16 * tb * D + (t16 ^ (ks << 3))), x, 0, 0, 0);
+          for (int ks = 0; ks < D / 32; ++ks) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ko[ks], qo[ks], x, 0, 0, 0);
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[r] = fac[i][r] != 0.f ? x[r] * fac[i][r] : 0.f;
           *reinterpret_cast<u32x2*>(Pl + Swizzled<C>::piece(16 * tb + l16, 2 * sb + (q4 >> 1)) + 4 * (q4 & 1)) =
@@ -209,6 +214,18 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
       }
     }
     __builtin_amdgcn_sched_barrier(0);           // (the rest's reads ahead of the scores would cost registers)
+    // (what a step's products read is asked for during the step before, the scores' all at once: 273 -> 264 us)
+    bf16x8 qn[4], qa[4], kc[4][G::IT];
+    auto read = [&](int ks) {
+      if (ks > 3) return;
+      if (!STATE_ONLY && ks < 2 * G::IT) {
+        qn[ks] = kv.rows(Ql, 32 * half, 2 * G::IT * half + ks);
+        qa[ks] = kv.rows(Ql, 32 * (1 - half), 2 * G::IT * half + ks);
+      }
+#pragma unroll
+      for (int it = 0; it < G::IT; ++it) kc[ks][it] = kx.cols(Kl, 16 * ks, G::IT * half + it);
+    };
+    read(0);
     // ---- S^T Q^T over this wave's rows of S: its own queries' and, for the other wave of the pair, that one's
     bf16x8 sop[2 * G::IT];
     if (!STATE_ONLY) {
@@ -224,9 +241,11 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
     O = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
+      __builtin_amdgcn_sched_barrier(0);
+      read(ks + 1);
       if (!STATE_ONLY && ks < 2 * G::IT) {
-        O = mfma(sop[ks], kv.rows(Ql, 32 * half, 2 * G::IT * half + ks), O);
-        away = mfma(sop[ks], kv.rows(Ql, 32 * (1 - half), 2 * G::IT * half + ks), away);
+        O = mfma(sop[ks], qn[ks], O);
+        away = mfma(sop[ks], qa[ks], away);
       }
       f32x16 x;                                  // eight values; split8 takes them from an accumulator
 #pragma unroll
@@ -238,13 +257,10 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
         for (int j = 0; j < 8; ++j) x[j] = x[j] - (float)vt[0][j] - (float)vt[1][j];
         vt[2] = pack8(x, 0);
       }
-      bf16x8 k[G::IT];
-#pragma unroll
-      for (int it = 0; it < G::IT; ++it) k[it] = kx.cols(Kl, 16 * ks, G::IT * half + it);
 #pragma unroll
       for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-        for (int it = 0; it < G::IT; ++it) S[it] = mfma(k[it], vt[i], S[it]);
+        for (int it = 0; it < G::IT; ++it) S[it] = mfma(kc[ks][it], vt[i], S[it]);
     }
     if (!STATE_ONLY) {
 #pragma unroll
