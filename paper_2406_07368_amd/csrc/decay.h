@@ -25,10 +25,11 @@ struct DecayArgs {
   const int32_t* lens;     // [B] or null
   const float* S_in;       // [B,H,d,d] or null (one role only)
   float* S_out;            // or null
-  float* ws;               // nseg > 1: [B*H][roles][nseg][d*d], the state before every segment
+  float* ws;               // nseg > 1: [B*H][roles][nseg * pieces][d*d], the state before every segment, or, with fold, what every piece adds
   int B, H, L;
   int nseg, seg_len;       // segments of seg_len tokens (a multiple of 64), in the order of the walk
-  int fold;                // few segments: the workspace holds what each adds, and each sums up those before it
+  int fold;                // few segments: each sums up what those before it add
+  int pieces, piece_len;   // of a segment in the first pass (1 without fold)
   float scale;
 };
 hipError_t launch_decay_first_pass_bf16(const DecayArgs& a, int d, hipStream_t s);

@@ -39,27 +39,32 @@ __global__ __launch_bounds__(256) void state_through_kernel(const float* from, f
 }
 
 // Up to so many segments every segment sums up for itself what those before it add (64 KB each at d = 128, from the L2 cache)
-// instead of a launch that does.
+// instead of a launch that does.  Where there are two, the first pass has one of them to do, and cuts it into two pieces.
 constexpr int kFold = 4;
 
 struct Plan {
-  int nseg, seg_len;
+  int nseg, seg_len, pieces;
   size_t bytes;
 };
-// A walk needs a compute unit (bf16 rows of 128: its two row buffers take 120 KB of LDS; rows of 64: half of one).
-// Where there are fewer walks the sequence is cut into segments of two groups or more, for one more read of K and V.
+// A walk needs a compute unit (bf16 rows of 128: its two row buffers take 120 KB of LDS; fp32: the matrix cores; rows of 64: half of
+// one).  Where there are fewer walks the sequence is cut into segments of two groups or more (fp32, whose groups take longer: one), for
+// one more read of K and V, if what that saves -- of `groups` steps all but 1/n, and half as many steps of the first pass -- makes up
+// for the second launch: some four steps of bf16 (d = 128, 120 walks in two segments: 44 us of 47 at 16 groups, but 30 of 27 at 8),
+// half a one of fp32.
 Plan plan(const linattn_decay_desc* d, int32_t L, int roles) {
-  Plan p{1, L, 0};
+  Plan p{1, L, 1, 0};
   const bool f32 = d->io_dtype == LINATTN_F32;
-  const int64_t walks = (int64_t)roles * d->B * d->H, room = (d->d == 128 ? 256 : 512) * (f32 ? 2 : 1);
-  const int groups = (L + 63) / 64;
+  const int64_t walks = (int64_t)roles * d->B * d->H, room = d->d == 128 ? 256 : 512;
+  const int groups = (L + 63) / 64, least = f32 ? 1 : 2;
   int64_t n = room / walks;
-  if (n > groups / (f32 ? 1 : 2)) n = groups / (f32 ? 1 : 2);
+  if (n > groups / least) n = groups / least;
   if (n > 64) n = 64;
+  if (2 * groups * n - 3 * groups < (f32 ? 1 : 8) * n) n = 1;
   if (n > 1) {
-    p.seg_len = (int)((groups + n - 1) / n) * 64;
+    p.pieces = n == 2 && groups >= 4 * least ? 2 : 1;
+    p.seg_len = (int)((groups + n * p.pieces - 1) / (n * p.pieces)) * 64 * p.pieces;
     p.nseg = (L + p.seg_len - 1) / p.seg_len;
-    if (p.nseg > 1) p.bytes = (size_t)walks * p.nseg * d->d * d->d * sizeof(float);
+    if (p.nseg > 1) p.bytes = (size_t)walks * p.nseg * p.pieces * d->d * d->d * sizeof(float);
   }
   return p;
 }
@@ -82,13 +87,14 @@ linattn_status check(const linattn_decay_desc* d, int32_t L, bool gradient, bool
 
 linattn_status run(DecayArgs& a, const linattn_decay_desc* d, const Plan& p, void* workspace, hipStream_t s) {
   a.B = d->B; a.H = d->H; a.scale = d->scale;
-  a.nseg = p.nseg; a.seg_len = p.seg_len; a.ws = static_cast<float*>(workspace);
+  a.nseg = p.nseg; a.seg_len = p.seg_len; a.pieces = 1; a.piece_len = p.seg_len; a.ws = static_cast<float*>(workspace);
   const bool bf16 = d->io_dtype == LINATTN_BF16;
   hipError_t e = hipSuccess;
   if (p.nseg > 1) {
-    e = bf16 ? launch_decay_first_pass_bf16(a, d->d, s) : launch_decay_first_pass_f32(a, d->d, s);
     // (in place: the last segment writes the state that the others would read)
     a.fold = p.nseg <= kFold && !(a.S_in && a.S_in == a.S_out);
+    a.pieces = a.fold ? p.pieces : 1; a.piece_len = p.seg_len / a.pieces;
+    e = bf16 ? launch_decay_first_pass_bf16(a, d->d, s) : launch_decay_first_pass_f32(a, d->d, s);
     if (e == hipSuccess && !a.fold) {
       const int dd = d->d * d->d;
       decay_scan_kernel<<<dim3(a.roles * a.B * a.H * (dd / 256)), 256, 0, s>>>(a, dd);

@@ -67,17 +67,18 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), ct = w % G::CT, half = w / G::CT;
   const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5, l16 = lane & 15, q4 = lane >> 4;
-  const int seg = blockIdx.x % a.nseg, bhr = blockIdx.x / a.nseg;
+  // first pass: the pieces of all segments but the last, behind which nothing starts
+  const int nseg = STATE_ONLY ? (a.nseg - 1) * a.pieces : a.nseg, seg_len = STATE_ONLY ? a.piece_len : a.seg_len;
+  const int seg = blockIdx.x % nseg, bhr = blockIdx.x / nseg;
   const int bh = bhr / a.roles, b = bh / a.H, h = bh % a.H;   // (the roles of a head side by side: they read the same rows)
   const DecayRole& role = a.role[bhr % a.roles];
   const int reverse = role.reverse;
   const Walk wq = walk(role.q, b, h), wk = walk(role.k, b, h), wv = walk(role.v, b, h), wo = walk(role.out, b, h);
   const int len = clamp_len(a.lens, b, a.L);
-  const int t_begin = seg * a.seg_len;
-  const int t_end = t_begin + a.seg_len < a.L ? t_begin + a.seg_len : a.L;
+  const int t_begin = seg * seg_len;
+  const int t_end = t_begin + seg_len < a.L ? t_begin + seg_len : a.L;
   const float g2 = decay_log2(a.log_decay, h);
-  float* slot = a.ws + ((size_t)bhr * a.nseg + seg) * (D * D);
-  if (STATE_ONLY && seg == a.nseg - 1) return;   // nothing starts behind the last segment
+  float* slots = a.ws + (size_t)bhr * a.nseg * a.pieces * (D * D);
 
   const int live_end = t_end < len ? t_end : len;                        // tokens that are there
   const int ng = live_end > t_begin ? (live_end - t_begin + C - 1) / C : 0;
@@ -107,15 +108,15 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
   auto row_of = [&](int r) { return 16 * (r >> 3) + 8 * hi + (r & 7); };
   auto at = [&](int it, int r) { return (32 * (G::IT * half + it) + row_of(r)) * D + 32 * ct + l32; };
   f32x16 S[G::IT];
-  const float* S0 = STATE_ONLY ? nullptr : a.nseg > 1 && !a.fold ? slot : a.S_in ? a.S_in + (size_t)bh * D * D : nullptr;
+  const float* S0 = STATE_ONLY ? nullptr : a.nseg > 1 && !a.fold ? slots + (size_t)seg * (D * D) : a.S_in ? a.S_in + (size_t)bh * D * D : nullptr;
 #pragma unroll
   for (int it = 0; it < G::IT; ++it)
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[it][r] = S0 ? S0[at(it, r)] : 0.f;
   if (!STATE_ONLY && a.nseg > 1 && a.fold) {     // few segments: what those before this one add, instead of a launch that sums it up
-    for (int j = 0; j < seg; ++j) {              // (four increments in flight at once: 40 registers spilled, 8 % slower)
-      const float* inc = a.ws + ((size_t)bhr * a.nseg + j) * (D * D);
-      const float keep = decay_pow(g2, segment_tokens(j, a.seg_len, len));
+    for (int j = 0; j < seg * a.pieces; ++j) {              // (four increments in flight at once: 40 registers spilled, 8 % slower)
+      const float* inc = slots + (size_t)j * (D * D);
+      const float keep = decay_pow(g2, segment_tokens(j, a.piece_len, len));
 #pragma unroll
       for (int it = 0; it < G::IT; ++it)
 #pragma unroll
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
       *reinterpret_cast<u32x4*>(gout + (int64_t)(t_begin + ng * C + e / G::PPR) * wo.t + e % G::PPR * 8) = z;
     }
   }
-  float* So = STATE_ONLY ? slot : a.S_out && seg == a.nseg - 1 ? a.S_out + (size_t)bh * D * D : nullptr;
+  float* So = STATE_ONLY ? slots + (size_t)seg * (D * D) : a.S_out && seg == a.nseg - 1 ? a.S_out + (size_t)bh * D * D : nullptr;
   if (So) {
 #pragma unroll
     for (int it = 0; it < G::IT; ++it)
@@ -315,7 +316,7 @@ hipError_t launch(const DecayArgs& a, hipStream_t s) {
   constexpr int bytes = STATE_ONLY ? G::KV : G::ALL;
   hipError_t e = LINATTN_MAX_LDS_ONCE((decay_prefill_kernel<D, STATE_ONLY, TERMS>), bytes);
   if (e != hipSuccess) return e;
-  decay_prefill_kernel<D, STATE_ONLY, TERMS><<<dim3(a.roles * a.B * a.H * a.nseg), G::NT, bytes, s>>>(a);
+  decay_prefill_kernel<D, STATE_ONLY, TERMS><<<dim3(a.roles * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.pieces : a.nseg)), G::NT, bytes, s>>>(a);
   return hipGetLastError();
 }
 

@@ -59,6 +59,34 @@ def test_prefill(dtype, B, H, L, d, state, ragged):
         assert not out.cpu().float().transpose(1, 2)[behind].any()
 
 
+@pytest.mark.parametrize("dtype,B,H,L,d,state", [
+    (BF, 2, 86, 1000, 64, True), (F32, 2, 86, 300, 64, True),      # two segments, the first summed up in two pieces
+    (BF, 2, 70, 520, 64, False), (BF, 1, 3, 520, 128, True), (F32, 1, 3, 256, 128, False), (BF, 1, 2, 4100, 64, True)])   # three, four, four, many
+def test_prefill_in_segments(dtype, B, H, L, d, state):
+    q, k, v = rows(B, H, L, d, dtype, 31)
+    g = slopes(H)
+    S0 = torch.randn((B, H, d, d), generator=torch.Generator().manual_seed(32)) if state else None
+    lens = torch.tensor([L, L // 4 + 9][:B], dtype=torch.int32)
+    want, S, size, A = plain(q.double(), k.double(), v.double(), g, 0.25, None if S0 is None else S0.double(), lens)
+    a = cuda(q, k, v, g, S0, lens)
+    out, Sg = binding.decay_prefill(a[0], a[1], a[2], a[3], 0.25, a[4], a[5])
+    near(out, want, size, dtype, ROUNDINGS[dtype], "out", NORM[dtype])
+    check_state(Sg, S, A, "S")
+
+
+@pytest.mark.parametrize("dtype,B,H,L,d", [(BF, 2, 30, 1000, 64), (F32, 2, 30, 400, 64)])
+def test_gradient_in_segments(dtype, B, H, L, d):
+    """A batch whose walks are cut in two against its rows alone, which are cut into more."""
+    q, k, v, do = cuda(*rows(B, H, L, d, dtype, 33, 4))
+    g, lens = cuda(slopes(H), torch.tensor([L, L // 4 + 9], dtype=torch.int32))
+    got = binding.decay_backward(q, k, v, g, do, lens=lens)
+    for b in range(B):
+        one = slice(b, b + 1)
+        for x, y in zip(got, binding.decay_backward(q[one], k[one], v[one], g, do[one], lens=lens[one].clone())):
+            # each is off by the roundings of three stages, together one U in the 2-norm (fp32: some hundred additions)
+            assert float((x[one].double() - y.double()).norm()) <= (2 * 2.0 ** -8 if dtype == BF else 1e-5) * float(y.double().norm())
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("L", [70, 400, 1500])                   # one segment, a few, many
 def test_state_in_place_and_no_tokens(dtype, L):
