@@ -23,6 +23,7 @@ struct WindowArgs {
   int B, H, Hkv, L;
   int window, sinks;
   float scale;
+  float dk_scale;                 // gradient: scale, or 0 where every token sees only itself
 };
 hipError_t launch_window_prefill_bf16(const WindowArgs& a, int d, hipStream_t s);
 hipError_t launch_window_prefill_f32(const WindowArgs& a, int d, hipStream_t s);

@@ -124,6 +124,7 @@ linattn_status linattn_window_backward(const linattn_window_desc* desc, int32_t 
   a.sink_part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_sinks);
   a.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
   a.far = p.far; a.parts = p.parts;
+  a.dk_scale = L == 1 || (desc->window == 1 && desc->sinks == 0) ? 0.f : desc->scale;
   return launch_window_backward(a, desc->d, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? LINATTN_OK : LINATTN_ERR_HIP;
 }
 

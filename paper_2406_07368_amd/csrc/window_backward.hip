@@ -107,7 +107,6 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
   }
   delta = add_xor32(delta);
   const float lse2 = a.lse[stat + tr] * 1.44269504088896340736f;
-  if (t < len) a.stats[hi * (int64_t)a.B * a.H * a.L + stat + t] = hi ? delta : lse2;
 
   const int last = (t_end < len ? t_end : len) - 1;
   const int lo = (t0 - a.window + 1 > 0 ? t0 - a.window + 1 : 0) / 64;
@@ -128,6 +127,41 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
     __syncthreads();
   };
   constexpr int AHEAD = 3;
+  auto visible = [&](int sw) { return sw <= tw + 31 && (sw + 31 > tw - a.window || sw < a.sinks); };
+  uint16_t *even = smem, *odd = smem + G::BUF;
+  // A row that sees n keys has an out of 1 / sqrt(n) of a value row, and so much of out's rounding to bf16 is in delta: where n is
+  // small the gradient would be off by more than all of its own roundings.  There delta is summed up from the weights, in a pass of
+  // its own over at most four key tiles (16 -> 18 us where a sequence has no other; nothing at the size above).
+  if (t0 == 0 || (int64_t)a.window + a.sinks < 64) {
+    float sum = 0.f;
+    auto turn = [&](int i, uint16_t* cur, uint16_t* next) {
+      arrive(i, cur);
+      if (i + 1 < nk) request(i + 1, next);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const int sw = key0(i) + 32 * kt;
+        if (!visible(sw)) continue;
+        f32x16 x = {}, y = {};
+#pragma unroll
+        for (int ks = 0; ks < G::KS; ++ks) {
+          x = mfma(lds.rows(cur, 32 * kt, ks), qop[ks], x);
+          y = mfma(lds.rows(cur + 64 * D, 32 * kt, ks), dop[ks], y);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (window_sees(t, sw + acc_row(r, hi), a.window, a.sinks)) sum += __builtin_amdgcn_exp2f(x[r] * c - lse2) * y[r];
+      }
+    };
+    request(0, even);
+    for (int i = 0; i < nk; ++i) turn(i, i % 2 ? odd : even, i % 2 ? even : odd);
+    __syncthreads();
+    delta = add_xor32(sum);
+  }
+  if (t < len) a.stats[hi * (int64_t)a.B * a.H * a.L + stat + t] = hi ? delta : lse2;
+
+  // The weight of a token that sees only itself is 1 whatever the score: no gradient, which dP - delta would give only up to its
+  // rounding.  (-1 sees nothing.  A tile with such a token is never one in which all is seen.)
+  const int tm = t == 0 || (a.window == 1 && a.sinks == 0) ? -1 : t;
   f32x16 dQ[G::CT];
 #pragma unroll
   for (int i = 0; i < G::CT; ++i) dQ[i] = f32x16{};
@@ -136,7 +170,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       const int sw = key0(i) + 32 * kt;
-      if (!(sw <= tw + 31 && (sw + 31 > tw - a.window || sw < a.sinks))) continue;
+      if (!visible(sw)) continue;
       // the matrix operands in the order of their use, AHEAD of each kind read before they are needed
       bf16x8 ko[G::KS], vo[G::KS], kt_op[2 * G::CT];
       auto read = [&](int j) {
@@ -170,7 +204,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
         if (!all) {
 #pragma unroll
           for (int r = 8 * half; r < 8 * half + 8; ++r)
-            if (!window_sees(t, sw + acc_row(r, hi), a.window, a.sinks)) x[r] = 0.f;
+            if (!window_sees(tm, sw + acc_row(r, hi), a.window, a.sinks)) x[r] = 0.f;
         }
         const bf16x8 p = pack8(x, 8 * half);
 #pragma unroll
@@ -189,7 +223,6 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a) {
     if (i + 1 < nk) request(i + 1, next);
     tile_of(i, cur);
   };
-  uint16_t *even = smem, *odd = smem + G::BUF;
   request(0, even);
   for (int i = 0; i < nk; i += 2) {
     turn(i, even, odd);
@@ -374,7 +407,7 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
     if (second.head < group) one(second, it, turn + 1, odd, stats + 2 * kWindowQ, even, stats);
   }
   if (!sink_job && a.parts == 1) {
-    store_tile<D>(smem, dK, a.scale, gdk, a.dk.t, s0, s_end, len, tid);
+    store_tile<D>(smem, dK, a.dk_scale, gdk, a.dk.t, s0, s_end, len, tid);
     store_tile<D>(smem, dV, 1.f, gdv, a.dv.t, s0, s_end, len, tid);
   }
   // where the sums of this lane's key go, if they are a share: [2][rows][D], dk then dv
@@ -424,7 +457,7 @@ __global__ __launch_bounds__(256) void window_shares_kernel(WindowArgs a) {
 #pragma unroll
     for (int i = 1; i < PER; ++i) x += *reinterpret_cast<const f32x4*>(&sum[i][e]);
   }
-  if (!kv) x *= a.scale;
+  if (!kv) x *= a.dk_scale;
   const Rows& o = kv ? a.dv : a.dk;
   uint16_t* out = const_cast<uint16_t*>(static_cast<const uint16_t*>(o.p)) + b * o.b + hk * o.h + row * o.t;
   *reinterpret_cast<u32x2*>(out + e) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};

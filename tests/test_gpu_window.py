@@ -143,6 +143,25 @@ def test_gradient(B, H, Hkv, L, d, W, sinks, ragged):
         near(g, w, s, BF, 1 if n == "v" else 2, "d" + n, 5e-3 if n == "v" or W > 8 else math.inf)
 
 
+@pytest.mark.parametrize("B,H,Hkv,L,d,W,sinks", [(19, 1, 1, 7, 128, 88, 1), (2, 4, 4, 117, 64, 3610, 0), (2, 24, 3, 85, 128, 10, 1), (2, 2, 1, 300, 64, 5, 2), (1, 4, 2, 200, 128, 2, 0),
+                                                  (3, 4, 1, 176, 64, 1, 0), (1, 2, 2, 140, 128, 1, 3),
+                                                  (5, 2, 1, 1, 64, 7, 1)])
+def test_gradient_of_rows_that_see_few_keys(B, H, Hkv, L, d, W, sinks):
+    q, do = rows(B, H, L, d, BF, 41, 2)
+    k, v = rows(B, Hkv, L, d, BF, 42, 2)
+    x = [t.double().requires_grad_() for t in (q, k, v)]
+    want = torch.autograd.grad(plain(*x, W, sinks, d ** -0.5)[0], x, do.double())
+    a = cuda(q, k, v, do)
+    out, lse, _ = binding.window_prefill(*a[:3], W, sinks, want_lse=True)
+    for n, g, w in zip("qkv", binding.window_backward(*a[:3], out, lse, a[3], W, sinks), want):
+        if (L == 1 or W == 1 and sinks == 0) and n != "v":
+            assert not g.any()                     # one key a row: the softmax is constant
+            continue
+        # two independent roundings to bf16 in the 2-norm, dS (or P) and the result: sqrt(2) of the result's alone, and 8 % for chance
+        once = float((w.to(BF).double() - w).norm())
+        assert float((g.double().cpu() - w).norm()) <= 1.08 * math.sqrt(2) * once, n
+
+
 def test_gradient_against_differences():
     """The derivative along a random direction against central differences of the definition in 64 bits."""
     B, H, Hkv, L, d, W, sinks, eps = 1, 4, 2, 200, 64, 50, 3, 1e-4
