@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256, M<D>::WAVES) void window_step_kernel(WindowSte
       float* stat = a.ws + (int64_t)a.B * a.Hkv * a.nsplit * R * D + 2 * at;
       if (hi == 0) { stat[0] = m; stat[1] = l; }
       float* o = a.ws + at * D;
-      if (l > 0.f) {
+      if (l != 0.f) {                                // (0: a share of nothing.  NaN is one of something)
 #pragma unroll
         for (int ct = 0; ct < D / 32; ++ct)
 #pragma unroll
@@ -333,22 +333,22 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowStepArgs a) {
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      st[i][0] = st[i][1] > 0.f ? __builtin_amdgcn_exp2f(st[i][0] - m) : 0.f;
+      st[i][0] = __builtin_amdgcn_exp2f(st[i][0] - m);
       l += st[i][1] * st[i][0];
     }
 #pragma unroll
     for (int d = 1; d < LR; d *= 2) l += __shfl_xor(l, d);
     const float inv = 1.f / l;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) weight[u][e + LR * i] = st[i][0] * inv;
+    for (int i = 0; i < EACH; ++i) weight[u][e + LR * i] = st[i][1] != 0.f ? st[i][0] * inv : -1.f;   // (-1: a share of nothing, which was not written)
     __syncthreads();
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int s = 0; s < a.nsplit; ++s) {
-      const float f = weight[u][s];                  // 0: a share of nothing, which was not written
+      const float f = weight[u][s];                  // (a weight that is NaN, or 0 for values that are, goes into the sum)
       const f32x4 y = *reinterpret_cast<const f32x4*>(a.ws + (at + (int64_t)s * R) * D + 4 * e);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] += f > 0.f ? f * y[i] : 0.f;
+      for (int i = 0; i < 4; ++i) x[i] += f < 0.f ? 0.f : f * y[i];
     }
     if (row < R) {
       E* o = static_cast<E*>(a.out) + (qrow + row) * D + 4 * e;
