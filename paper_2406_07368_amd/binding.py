@@ -623,10 +623,17 @@ def _kv(where, q, k, v, window, sinks):
         raise ValueError(f"{where}: k and v must have one shape, q's with a number of heads that divides q's")
 
 
-def window_cache(B, H_kv, d, window, sinks=0, dtype=torch.bfloat16, device="cuda"):
-    """Cache of ``window_step`` for sequences that have not begun: (kcache, vcache, pos)."""
+def _new_cache(B, H_kv, d, window, sinks, dtype, device):
+    """Memory alone: no kernel of torch's, which would run on the current stream whatever stream the call is for."""
     rows = [torch.empty((B, H_kv, sinks + window, d), dtype=dtype, device=device) for _ in range(2)]
-    return (*rows, torch.zeros((B, H_kv), dtype=torch.int32, device=device))
+    return (*rows, torch.empty((B, H_kv), dtype=torch.int32, device=device))
+
+
+def window_cache(B, H_kv, d, window, sinks=0, dtype=torch.bfloat16, device="cuda"):
+    """Cache of ``window_step`` for sequences that have not begun: (kcache, vcache, pos).  (pos is cleared on the current stream.)"""
+    cache = _new_cache(B, H_kv, d, window, sinks, dtype, device)
+    cache[2].zero_()
+    return cache
 
 
 def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=False, want_cache=False, stream=None):
@@ -647,7 +654,7 @@ def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=Fal
     with _on(q.device):
         out = _like(q)
         lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
-        cache = window_cache(B, k.shape[1], d, window, sinks, q.dtype, q.device) if want_cache else None
+        cache = _new_cache(B, k.shape[1], d, window, sinks, q.dtype, q.device) if want_cache else None   # (the call writes every pos)
         desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v), out=_st(out))
         linattn_window_prefill(desc, L, q, k, v, lens, out, lse, *(cache or (None, None, None)), stream)
     return out, lse, cache

@@ -62,3 +62,31 @@ def test_step_hands_on_what_is_not_finite(dtype, B, H, Hkv, d, kk, W, sinks, pos
     assert torch.equal(got[1:], want[1:]) and torch.equal(got[:, others], want[:, others])
     if where == "query":
         assert bool(torch.isfinite(got.cpu()[~hit]).all())
+
+
+def keep_busy():
+    """Some 50 ms of work on the current stream."""
+    x = torch.ones((8192, 8192), dtype=BF, device="cuda")
+    for _ in range(60):
+        x @ x
+
+
+@pytest.mark.parametrize("L", [90, 0])
+def test_cache_of_a_prompt_on_another_stream(L):
+    """Nothing of the call runs on the current stream, which is behind: pos says how long the prompts are."""
+    B, H, Hkv, d, W, sinks = 3, 4, 2, 64, 40, 2
+    q, = cuda(*rows(B, H, L, d, BF, 61))
+    k, v = cuda(*rows(B, Hkv, L, d, BF, 62, 2))
+    tok = cuda(*rows(B, H, 1, d, BF, 63), *rows(B, Hkv, 1, d, BF, 64, 2))
+    lens = torch.tensor([L, L // 3, 0], dtype=torch.int32, device="cuda")
+    _, _, cache = binding.window_prefill(q, k, v, W, sinks, lens=lens, want_cache=True)
+    assert cache[2].tolist() == [[n] * Hkv for n in lens.tolist()]
+    want = binding.window_step(*tok, cache, W, sinks)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    keep_busy()
+    _, _, cache = binding.window_prefill(q, k, v, W, sinks, lens=lens, want_cache=True, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert cache[2].tolist() == [[n] * Hkv for n in lens.tolist()]
+    assert torch.equal(binding.window_step(*tok, cache, W, sinks), want)
