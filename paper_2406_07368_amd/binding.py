@@ -11,6 +11,7 @@ cannot be built or loaded they are marshalled here, and a warning says so once.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import warnings
@@ -360,6 +361,35 @@ def linattn_window_step(desc: WindowDesc, kk, q, k, v, kcache, vcache, pos, n_co
 
 
 # ---- conveniences that only allocate with torch and forward to the calls above ---------------
+# ``stream``: None for the current one, or a torch stream or a raw handle on which the call is enqueued.  What the call reads has to
+# be ready for that stream, and what it returns is ready when that stream is done, as usual between streams; no memory that
+# the call works on is handed out again before it is done, whatever becomes of the tensors.
+@contextlib.contextmanager
+def _memory_for(stream, device, *given):
+    """Marks the tensors that the call is given as in use by ``stream``.  What is allocated in here belongs to it: memory that earlier
+    work of another stream may still use is not taken, and a workspace that is let go is handed out again only behind the call.  Yields
+    what marks a tensor that is returned: the caller's current stream uses it too."""
+    if stream is None:
+        yield lambda t: t
+        return
+    caller = torch.cuda.current_stream(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream if isinstance(stream, int) else stream.cuda_stream
+        # (0, and 1 by its other name: the default stream, which ExternalStream does not take)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle not in (0, 1) else torch.cuda.default_stream(device)
+
+    def returned(t):
+        if t is not None:
+            t.record_stream(caller)
+        return t
+
+    with torch.cuda.stream(stream):
+        for t in given:
+            if t is not None:
+                t.record_stream(stream)
+        yield returned
+
+
 def prefill(q, k, v, conv_w, state=None, chunk=64, eps=0.0, want_state=True, stream=None, phi="elu1", grouped_alpha=None):
     """q, k: [B,H,L,d], v: [B,H,L,d_v] CUDA tensors (fp32 or bf16; d_v = d or a multiple of d), dense or any view
     with unit stride along the last axis (e.g. ``x.transpose(1, 2)`` of a token-major [B,L,H,d] tensor); q and k
@@ -381,21 +411,20 @@ def prefill(q, k, v, conv_w, state=None, chunk=64, eps=0.0, want_state=True, str
         desc = make_desc(B, H, d, Kc, chunk, q.dtype, eps, strides=sq, L=L, phi=phi)
     else:
         desc = make_desc(B, H, d, Kc, chunk, q.dtype, eps, strides=sq, L=L, phi=phi, d_v=d_v, strides_v=sv)
-    out = torch.empty_like(v) if dense else torch.empty_strided(v.shape, v.stride(), dtype=v.dtype, device=v.device)
     S_in, z_in, h_in = state if state is not None else (None, None, None)
     S = z = h = None
-    if want_state:
-        S = torch.empty((B, H, d, d_v), dtype=torch.float32, device=q.device)
-        z = torch.empty((B, H, d), dtype=torch.float32, device=q.device)
-        h = torch.empty((B, H, max(Kc - 1, 0), d_v), dtype=q.dtype, device=q.device)
-    nbytes = linattn_workspace_bytes(desc, L)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
-    if ws is not None and stream is not None and not isinstance(stream, int):
-        ws.record_stream(stream)     # the allocator must not hand this memory out again before the launch stream is done with it
-    if grouped_alpha is None:
-        linattn_prefill(desc, L, q, k, v, conv_w, S_in, z_in, h_in, out, S, z, h, ws, nbytes, stream)
-    else:
-        linattn_prefill_grouped(desc, L, grouped_alpha, q, k, v, conv_w, S_in, z_in, h_in, out, S, z, h, ws, nbytes, stream)
+    with _memory_for(stream, q.device, q, k, v, conv_w, S_in, z_in, h_in) as returned:
+        out = returned(torch.empty_like(v) if dense else torch.empty_strided(v.shape, v.stride(), dtype=v.dtype, device=v.device))
+        if want_state:
+            S = returned(torch.empty((B, H, d, d_v), dtype=torch.float32, device=q.device))
+            z = returned(torch.empty((B, H, d), dtype=torch.float32, device=q.device))
+            h = returned(torch.empty((B, H, max(Kc - 1, 0), d_v), dtype=q.dtype, device=q.device))
+        nbytes = linattn_workspace_bytes(desc, L)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+        if grouped_alpha is None:
+            linattn_prefill(desc, L, q, k, v, conv_w, S_in, z_in, h_in, out, S, z, h, ws, nbytes, stream)
+        else:
+            linattn_prefill_grouped(desc, L, grouped_alpha, q, k, v, conv_w, S_in, z_in, h_in, out, S, z, h, ws, nbytes, stream)
     return out, (S, z, h)
 
 
@@ -421,13 +450,12 @@ def prefill_grouped_backward(q, k, v, conv_w, dout, alpha=1.0, eps=0.0, stream=N
         raise ValueError("q, k, v and dout must share their strides and be contiguous along d")
     desc = make_desc(B, H, d, Kc, group, q.dtype, eps, strides=None if dense else q.stride()[:3], L=L, phi=phi)
     new = (lambda: torch.empty_like(q)) if dense else (lambda: torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device))
-    dq, dk, dv = new(), new(), new()
-    dw = torch.empty((H, d, Kc), dtype=torch.float32, device=q.device) if want_dw else None
-    nbytes = linattn_backward_workspace_bytes(desc, L)
-    ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
-    if stream is not None and not isinstance(stream, int):
-        ws.record_stream(stream)
-    linattn_prefill_grouped_backward(desc, L, alpha, q, k, v, conv_w, dout, dq, dk, dv, dw, ws, nbytes, stream)
+    with _memory_for(stream, q.device, q, k, v, conv_w, dout) as returned:
+        dq, dk, dv = returned(new()), returned(new()), returned(new())
+        dw = returned(torch.empty((H, d, Kc), dtype=torch.float32, device=q.device)) if want_dw else None
+        nbytes = linattn_backward_workspace_bytes(desc, L)
+        ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        linattn_prefill_grouped_backward(desc, L, alpha, q, k, v, conv_w, dout, dq, dk, dv, dw, ws, nbytes, stream)
     return dq, dk, dv, dw
 
 
@@ -439,9 +467,10 @@ def verify(q, k, v, conv_w, state, n_commit=None, eps=0.0, stream=None, phi="elu
             return _result(r, "linattn_verify")
     B, H, kk, d = q.shape
     desc = make_desc(B, H, d, conv_w.shape[2], 64, q.dtype, eps, L=kk, phi=phi, d_v=v.shape[-1])
-    out = torch.empty_like(v)
     S, z, h = state
-    linattn_verify(desc, kk, q, k, v, conv_w, S, z, h, n_commit, out, stream)
+    with _memory_for(stream, q.device, q, k, v, conv_w, S, z, h, n_commit) as returned:
+        out = returned(torch.empty_like(v))
+        linattn_verify(desc, kk, q, k, v, conv_w, S, z, h, n_commit, out, stream)
     return out
 
 
@@ -469,9 +498,10 @@ def verify_grouped(q, k, v, conv_w, state, alpha=1.0, n_commit=None, eps=0.0, st
             return _result(r, "linattn_verify_grouped")
     B, H, kk, d = q.shape
     desc = make_desc(B, H, d, conv_w.shape[2], 64, q.dtype, eps, L=kk, phi=phi)
-    out = torch.empty_like(q)
     S, z, h, kwin, vwin, fill = state
-    linattn_verify_grouped(desc, kk, alpha, q, k, v, conv_w, S, z, h, kwin, vwin, fill, n_commit, out, stream)
+    with _memory_for(stream, q.device, q, k, v, conv_w, *state, n_commit) as returned:
+        out = returned(torch.empty_like(q))
+        linattn_verify_grouped(desc, kk, alpha, q, k, v, conv_w, S, z, h, kwin, vwin, fill, n_commit, out, stream)
     return out
 
 
@@ -484,9 +514,10 @@ def verify_tree(q, k, v, parent, conv_w, state, accept=None, eps=0.0, stream=Non
             return _result(r, "linattn_verify_tree")
     B, H, n, d = q.shape
     desc = make_desc(B, H, d, conv_w.shape[2], 64, q.dtype, eps, L=n, phi=phi)
-    out = torch.empty_like(q)
     S, z, h = state
-    linattn_verify_tree(desc, n, q, k, v, parent, conv_w, S, z, h, accept, out, stream)
+    with _memory_for(stream, q.device, q, k, v, parent, conv_w, S, z, h, accept) as returned:
+        out = returned(torch.empty_like(q))
+        linattn_verify_tree(desc, n, q, k, v, parent, conv_w, S, z, h, accept, out, stream)
     return out
 
 
@@ -498,9 +529,10 @@ def decode(q, k, v, conv_w, state, eps=0.0, stream=None, phi="elu1"):
             return _result(r, "linattn_decode")
     B, H, d = q.shape[0], q.shape[1], q.shape[-1]
     desc = make_desc(B, H, d, conv_w.shape[2], 64, q.dtype, eps, L=1, phi=phi, d_v=v.shape[-1])
-    out = torch.empty_like(v)
     S, z, h = state
-    linattn_decode(desc, q, k, v, conv_w, S, z, h, out, stream)
+    with _memory_for(stream, q.device, q, k, v, conv_w, S, z, h) as returned:
+        out = returned(torch.empty_like(v))
+        linattn_decode(desc, q, k, v, conv_w, S, z, h, out, stream)
     return out
 
 
@@ -531,11 +563,8 @@ def _like(x):
     return torch.empty_like(x)
 
 
-def _scratch(nbytes, device, stream):
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    if ws is not None and stream is not None and not isinstance(stream, int):
-        ws.record_stream(stream)
-    return ws
+def _scratch(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 def _on(device):
@@ -564,11 +593,11 @@ def decay_prefill(q, k, v, log_decay, scale=None, state=None, lens=None, want_st
     _aux("decay_prefill", "log_decay", log_decay, torch.float32, (H,), q.device)
     _aux("decay_prefill", "state", state, torch.float32, (B, H, d, d), q.device)
     _aux("decay_prefill", "lens", lens, torch.int32, (B,), q.device)
-    with _on(q.device):
-        out = _like(q)
-        S = torch.empty((B, H, d, d), dtype=torch.float32, device=q.device) if want_state else None
+    with _on(q.device), _memory_for(stream, q.device, q, k, v, log_decay, state, lens) as returned:
+        out = returned(_like(q))
+        S = returned(torch.empty((B, H, d, d), dtype=torch.float32, device=q.device)) if want_state else None
         desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v), out=_st(out))
-        ws = _scratch(linattn_decay_workspace_bytes(desc, L), q.device, stream)
+        ws = _scratch(linattn_decay_workspace_bytes(desc, L), q.device)
         linattn_decay_prefill(desc, L, q, k, v, log_decay, lens, state, out, S, ws, None, stream)
     return out, S
 
@@ -586,11 +615,11 @@ def decay_backward(q, k, v, log_decay, dout, scale=None, lens=None, stream=None)
         raise ValueError("decay_backward: q, k, v and dout must have one shape")
     _aux("decay_backward", "log_decay", log_decay, torch.float32, (H,), q.device)
     _aux("decay_backward", "lens", lens, torch.int32, (B,), q.device)
-    with _on(q.device):
-        dq, dk, dv = _like(q), _like(k), _like(v)
+    with _on(q.device), _memory_for(stream, q.device, q, k, v, log_decay, dout, lens) as returned:
+        dq, dk, dv = (returned(_like(x)) for x in (q, k, v))
         desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v),
                                dout=_st(dout), dq=_st(dq), dk=_st(dk), dv=_st(dv))
-        ws = _scratch(linattn_decay_backward_workspace_bytes(desc, L), q.device, stream)
+        ws = _scratch(linattn_decay_backward_workspace_bytes(desc, L), q.device)
         linattn_decay_backward(desc, L, q, k, v, log_decay, lens, dout, dq, dk, dv, ws, None, stream)
     return dq, dk, dv
 
@@ -609,8 +638,8 @@ def decay_step(q, k, v, log_decay, state, scale=None, n_commit=None, stream=None
     _aux("decay_step", "log_decay", log_decay, torch.float32, (H,), q.device)
     _aux("decay_step", "state", state, torch.float32, (B, H, d, d), q.device)
     _aux("decay_step", "n_commit", n_commit, torch.int32, (B,), q.device)
-    with _on(q.device):
-        out = torch.empty_like(q)
+    with _on(q.device), _memory_for(stream, q.device, q, k, v, log_decay, state, n_commit) as returned:
+        out = returned(torch.empty_like(q))
         desc = make_decay_desc(B, H, d, q.dtype, d ** -0.5 if scale is None else scale)
         linattn_decay_step(desc, kk, q, k, v, log_decay, state, n_commit, out, stream)
     return out
@@ -651,10 +680,10 @@ def window_prefill(q, k, v, window, sinks=0, scale=None, lens=None, want_lse=Fal
     _kv("window_prefill", q, k, v, window, sinks)
     B, H, L, d = q.shape
     _aux("window_prefill", "lens", lens, torch.int32, (B,), q.device)
-    with _on(q.device):
-        out = _like(q)
-        lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
-        cache = _new_cache(B, k.shape[1], d, window, sinks, q.dtype, q.device) if want_cache else None   # (the call writes every pos)
+    with _on(q.device), _memory_for(stream, q.device, q, k, v, lens) as returned:
+        out = returned(_like(q))
+        lse = returned(torch.empty((B, H, L), dtype=torch.float32, device=q.device)) if want_lse else None
+        cache = tuple(returned(x) for x in _new_cache(B, k.shape[1], d, window, sinks, q.dtype, q.device)) if want_cache else None   # (the call writes every pos)
         desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v), out=_st(out))
         linattn_window_prefill(desc, L, q, k, v, lens, out, lse, *(cache or (None, None, None)), stream)
     return out, lse, cache
@@ -676,11 +705,11 @@ def window_backward(q, k, v, out, lse, dout, window, sinks=0, scale=None, lens=N
         raise ValueError("window_backward: lse is what window_prefill returns with want_lse=True")
     _aux("window_backward", "lse", lse, torch.float32, (B, H, L), q.device)
     _aux("window_backward", "lens", lens, torch.int32, (B,), q.device)
-    with _on(q.device):
-        dq, dk, dv = _like(q), _like(k), _like(v)
+    with _on(q.device), _memory_for(stream, q.device, q, k, v, out, lse, dout, lens) as returned:
+        dq, dk, dv = (returned(_like(x)) for x in (q, k, v))
         desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale, q=_st(q), k=_st(k), v=_st(v),
                                 out=_st(out), dout=_st(dout), dq=_st(dq), dk=_st(dk), dv=_st(dv))
-        ws = _scratch(linattn_window_backward_workspace_bytes(desc, L), q.device, stream)
+        ws = _scratch(linattn_window_backward_workspace_bytes(desc, L), q.device)
         linattn_window_backward(desc, L, q, k, v, lens, out, lse, dout, dq, dk, dv, ws, None, stream)
     return dq, dk, dv
 
@@ -704,9 +733,9 @@ def window_step(q, k, v, cache, window, sinks=0, scale=None, n_commit=None, stre
         _aux("window_step", n, x, q.dtype, (B, k.shape[1], sinks + window, d), q.device)
     _aux("window_step", "pos", pos, torch.int32, (B, k.shape[1]), q.device)
     _aux("window_step", "n_commit", n_commit, torch.int32, (B,), q.device)
-    with _on(q.device):
-        out = torch.empty_like(q)
+    with _on(q.device), _memory_for(stream, q.device, q, k, v, kcache, vcache, pos, n_commit) as returned:
+        out = returned(torch.empty_like(q))
         desc = make_window_desc(B, H, k.shape[1], d, window, sinks, q.dtype, d ** -0.5 if scale is None else scale)
-        ws = _scratch(linattn_window_step_workspace_bytes(desc, kk), q.device, stream)
+        ws = _scratch(linattn_window_step_workspace_bytes(desc, kk), q.device)
         linattn_window_step(desc, kk, q, k, v, kcache, vcache, pos, n_commit, out, ws, None, stream)
     return out

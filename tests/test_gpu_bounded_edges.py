@@ -90,3 +90,76 @@ def test_cache_of_a_prompt_on_another_stream(L):
     torch.cuda.synchronize()
     assert cache[2].tolist() == [[n] * Hkv for n in lens.tolist()]
     assert torch.equal(binding.window_step(*tok, cache, W, sinks), want)
+
+
+def calls_for_a_stream():
+    """Calls that need a workspace, and calls that need none, of every kind; what each is given; as functions of the stream."""
+    B, H, d, L, W = 1, 4, 64, 900, 1200
+    q, k, v, do = cuda(*rows(B, H, L, d, BF, 71, 4))
+    tok = cuda(*rows(B, H, 3, d, BF, 72, 3))
+    held = cuda(*rows(B, H, W + 2, d, BF, 73, 2))
+    g, w = torch.linspace(-1, -0.01, H, device="cuda"), torch.rand(H, d, 3, device="cuda")
+    S, z, h = torch.randn(B, H, d, d, device="cuda"), torch.rand(B, H, d, device="cuda") + 9, cuda(*rows(B, H, 2, d, BF, 74))[0]
+    parent = torch.tensor([-1, 0, 0], dtype=torch.int32, device="cuda")
+    pos = torch.full((B, H), 3000, dtype=torch.int32, device="cuda")
+    out, lse, _ = binding.window_prefill(q, k, v, W, 2, want_lse=True)
+    x = dict(q=q, k=k, v=v, do=do, tq=tok[0], tk=tok[1], tv=tok[2], kc=held[0], vc=held[1], g=g, w=w, S=S, z=z, h=h, parent=parent, pos=pos, out=out, lse=lse)
+    x.update({n + "512": x[n][:, :, :512].contiguous() for n in ("q", "k", "v", "do")} | {n + "1": x["t" + n][:, :, 0].contiguous() for n in "qkv"})
+
+    def flat(r):
+        return [y for x in r if x is not None for y in (flat(x) if isinstance(x, tuple) else [x])] if isinstance(r, tuple) else [r]
+
+    return x, [lambda x, s, f=f: flat(f(x, s)) for f in (
+        lambda x, s: binding.decay_prefill(x["q"], x["k"], x["v"], x["g"], state=x["S"], stream=s),
+        lambda x, s: binding.decay_backward(x["q"], x["k"], x["v"], x["g"], x["do"], stream=s),
+        lambda x, s: (binding.decay_step(x["tq"], x["tk"], x["tv"], x["g"], x["S"], stream=s), x["S"]),
+        lambda x, s: binding.window_prefill(x["q"], x["k"], x["v"], W, 2, want_lse=True, stream=s),
+        lambda x, s: (lambda r: (r[0], r[2][0][:, :, :L], r[2][1][:, :, :L], r[2][2]))(binding.window_prefill(x["q"], x["k"], x["v"], W, 2, want_cache=True, stream=s)),
+        lambda x, s: binding.window_backward(x["q"], x["k"], x["v"], x["out"], x["lse"], x["do"], W, 2, stream=s),
+        lambda x, s: (binding.window_step(x["tq"], x["tk"], x["tv"], (x["kc"], x["vc"], x["pos"]), W, 2, stream=s), x["kc"], x["vc"], x["pos"]),
+        lambda x, s: binding.prefill(x["q"], x["k"], x["v"], x["w"], stream=s),
+        lambda x, s: binding.prefill_grouped_backward(x["q512"], x["k512"], x["v512"], x["w"], x["do512"], group=64, stream=s),
+        lambda x, s: (binding.verify(x["tq"], x["tk"], x["tv"], x["w"], (x["S"], x["z"], x["h"]), stream=s), x["S"], x["z"], x["h"]),
+        lambda x, s: binding.verify_tree(x["tq"], x["tk"], x["tv"], x["parent"], x["w"], (x["S"], x["z"], x["h"]), stream=s),
+        lambda x, s: binding.decode(x["q1"], x["k1"], x["v1"], x["w"], (x["S"], x["z"], x["h"]), stream=s))]
+
+
+def test_memory_of_calls_on_a_stream():
+    """Calls that wait on a busy stream, by its handle and as torch's: what they were given, their workspace and what they return is not
+    handed out to the stream that goes on, which fills whatever memory it gets."""
+    x, calls = calls_for_a_stream()
+    copies = lambda: {n: t.clone() for n, t in x.items()}  # noqa: E731
+    want = [[y.clone() for y in f(copies(), None)] for f in calls]
+    side = torch.cuda.Stream()
+    for handle in (side.cuda_stream, side):
+        for i, f in enumerate(calls):
+            given = copies()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                keep_busy()
+            got = f(given, handle)
+            sizes = [t.numel() * t.element_size() for t in given.values()]
+            del given
+            spoilt = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes + [1 << e for e in range(9, 24)] for _ in range(2)]
+            torch.cuda.synchronize()
+            assert len(got) == len(want[i]) and all(torch.equal(a, b) for a, b in zip(got, want[i])), i
+            del spoilt, got
+
+
+def test_memory_that_the_current_stream_still_uses():
+    """A call on an idle stream, while the current stream is behind and will still write to memory that was let go."""
+    x, calls = calls_for_a_stream()
+    copies = lambda: {n: t.clone() for n, t in x.items()}  # noqa: E731
+    want = [[y.clone() for y in f(copies(), None)] for f in calls]
+    side = torch.cuda.Stream()
+    for handle in (side.cuda_stream, side, 0):
+        for i, f in enumerate(calls):
+            given = copies()
+            torch.cuda.synchronize()
+            if handle != 0:
+                keep_busy()
+            for n in [t.numel() * t.element_size() for w in want for t in w] + [1 << e for e in range(9, 24)]:
+                torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+            got = f(given, handle)
+            torch.cuda.synchronize()
+            assert len(got) == len(want[i]) and all(torch.equal(a, b) for a, b in zip(got, want[i])), i
