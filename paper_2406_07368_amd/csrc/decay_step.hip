@@ -1,7 +1,7 @@
 // kk tokens of linear attention with a decay, from a running state (fp32 throughout).  With lambda the head's decay,
 //
 //   out_j = scale ( lambda^{j+1} q_j^T S + sum_{i<=j} lambda^{j-i} (q_j.k_i) v_i )
-//   S'    = lambda^n S + sum_{i<n} lambda^{n-1-i} k_i v_i^T                          n = drafts that are kept
+//   S'    = lambda^n S + sum_{i<n} lambda^{n-1-i} k_i v_i^T                          n = drafts that are kept (see Fade)
 //
 // One read and one write of the state (8 d^2 bytes a head) is all the traffic that counts: HBM bounds it.  Every value
 // column is independent of the others, so a workgroup takes CB columns of one head: a thread holds R rows of four
@@ -17,8 +17,9 @@ namespace linattn {
 
 namespace {
 
+// (eight waves on a SIMD, where LDS has room for them: left alone the compiler takes registers for five, 27.5 -> 27.8 us)
 template <typename IO, int D, int CB, int KK>
-__global__ __launch_bounds__(256) void decay_step_kernel(DecayStepArgs a) {
+__global__ __launch_bounds__(256, KK <= 8 ? 8 : 5) void decay_step_kernel(DecayStepArgs a) {
   constexpr int LG = CB / 4;              // lanes side by side on a row's columns
   constexpr int NG = 256 / LG;            // row groups
   constexpr int R = D / NG;               // rows of S per thread
@@ -52,6 +53,7 @@ __global__ __launch_bounds__(256) void decay_step_kernel(DecayStepArgs a) {
     n = a.n_commit[b];
     n = n < 0 ? 0 : n > kk ? kk : n;
   }
+  const Fade fade(a.log_decay, h, n);
   __syncthreads();
   // q_j . k_i, eight lanes each
   for (int p = tid >> 3; p < KK * KK; p += 32) {
@@ -88,14 +90,17 @@ __global__ __launch_bounds__(256) void decay_step_kernel(DecayStepArgs a) {
     }
   }
   if (n == 0) return;
-  const float keep = decay_pow(g2, n);
+  // what the state loses and gains goes into it in one rounding (a loss of less than 2^-25 of it would be lost alone)
+  f32x4 more[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) s[r] *= keep;
+  for (int r = 0; r < R; ++r) more[r] = s[r] * fade.f;
   for (int i = 0; i < n; ++i) {
     const f32x4 x = *reinterpret_cast<const f32x4*>(&vl[i][c]) * decay_pow(g2, n - 1 - i);
 #pragma unroll
-    for (int r = 0; r < R; ++r) s[r] += kl[i][g + NG * r] * x;
+    for (int r = 0; r < R; ++r) more[r] += kl[i][g + NG * r] * x;
   }
+#pragma unroll
+  for (int r = 0; r < R; ++r) s[r] = fade.slow ? s[r] + more[r] : more[r];
 #pragma unroll
   for (int r = 0; r < R; ++r) *reinterpret_cast<f32x4*>(S + (size_t)(g + NG * r) * D) = s[r];
 }

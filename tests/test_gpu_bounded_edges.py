@@ -163,3 +163,29 @@ def test_memory_that_the_current_stream_still_uses():
             got = f(given, handle)
             torch.cuda.synchronize()
             assert len(got) == len(want[i]) and all(torch.equal(a, b) for a, b in zip(got, want[i])), i
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kk,keep", [(1, 1), (4, 3)])
+def test_thousands_of_steps(dtype, kk, keep):
+    """Decays that no 32-bit factor near 1 meets exactly, on rows whose state only grows, against the recurrence in 64 bits."""
+    g = torch.tensor([-1.3 * 2 ** -11, -1.3 * 2 ** -10, -1e-3, -1.7e-5, -0.03, -2.0, 0.0])
+    B, H, d, n = 1, len(g), 64, 4096
+    k, v = (torch.rand((n, B, H, kk, d), generator=torch.Generator().manual_seed(54 + i)).to(dtype).cuda() for i in range(2))
+    gg, commit = g.cuda(), torch.full((B,), keep, dtype=torch.int32, device="cuda")
+    S = torch.zeros((B, H, d, d), device="cuda")
+    for t in range(n):
+        binding.decay_step(k[t], k[t], v[t], gg, S, 1.0, commit)
+    lam = torch.exp(g.double()).cuda()[:, None, None]
+    want = torch.zeros((B, H, d, d), dtype=torch.float64, device="cuda")
+    for t in range(n):
+        for i in range(keep):
+            want = lam * want + k[t, :, :, i, :, None].double() * v[t, :, :, i, None, :].double()
+    for h in range(H):
+        # A step rounds the sum of a state and what it gains, by at most 2^-24 of it and 2^-24 / sqrt(3) in the mean square,
+        # independently of the others'; it weighs lambda^keep to the power of the steps that follow.  Twice that, for the
+        # gain's own roundings and chance, and 2^-22 for the factor (1 - lambda), which is off by some 2^-23 of itself.
+        lam2 = math.exp(2 * keep * float(g[h]))
+        steps = n if lam2 == 1 else min(n, 1 / (1 - lam2))
+        rel = float((S[0, h].double() - want[0, h]).norm() / want[0, h].norm())
+        assert rel <= 2 * 2.0 ** -24 / math.sqrt(3) * math.sqrt(steps) + 2.0 ** -22, (float(g[h]), rel)
