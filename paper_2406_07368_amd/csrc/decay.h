@@ -54,12 +54,6 @@ __device__ __forceinline__ float decay_log2(const float* log_decay, int h) {
   const float g = log_decay[h] * 1.44269504088896340736f;
   return g < 0.f ? fmaxf(g, -1e30f) : 0.f;
 }
-// lambda^n - 1, n >= 0, for a state that decays by it once a group: x + x (lambda^n - 1).  A factor near 1 held as such is off by
-// 2^-24, always to the same side, and a slow head's state meets it dozens of times.
-__device__ __forceinline__ float decay_pow_less_1(const float* log_decay, int h, int n) {
-  const float g = log_decay[h];
-  return g < 0.f ? expm1f(fmaxf(g, -1e30f) * (float)n) : 0.f;
-}
 // What a running state x becomes over n >= 0 tokens: slow ? x + x f : x f.  A factor near 1 held as such is off by up to 2^-24, always
 // to the same side, and a state that lives through thousands of steps of a slow head meets it in every one of them: lambda^n - 1 has
 // all its bits.  Where lambda^n is 1/2 or less the difference would cancel, and what is left of the state is right by its factor.
@@ -67,10 +61,11 @@ struct Fade {
   float f;
   bool slow;
   __device__ __forceinline__ Fade(const float* log_decay, int h, int n) {
-    const float less = decay_pow_less_1(log_decay, h, n);
+    const float g = log_decay[h], less = g < 0.f ? expm1f(fmaxf(g, -1e30f) * (float)n) : 0.f;
     slow = less > -0.5f;
     f = slow ? less : __builtin_amdgcn_exp2f(decay_log2(log_decay, h) * (float)n);
   }
+  __device__ __forceinline__ float of(float x) const { return slow ? x + x * f : x * f; }
 };
 // lambda^n, n >= 0
 __device__ __forceinline__ float decay_pow(float g2, int n) { return __builtin_amdgcn_exp2f(g2 * (float)n); }

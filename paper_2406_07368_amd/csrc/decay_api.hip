@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int dd) {
   const int per = dd / 256, bhr = blockIdx.x / per, e = blockIdx.x % per * 256 + threadIdx.x;
   const int bh = bhr / a.roles, b = bh / a.H;
   const int len = clamp_len(a.lens, b, a.L);
-  const float g2 = decay_log2(a.log_decay, bh % a.H);
+  const Fade whole(a.log_decay, bh % a.H, a.seg_len), end(a.log_decay, bh % a.H, len % a.seg_len);   // (over a segment; over the one that the sequence ends in)
   float* p = a.ws + (size_t)bhr * a.nseg * dd + e;
   float x = a.S_in ? a.S_in[(size_t)bh * dd + e] : 0.f;
   for (int s0 = 0; s0 < a.nseg; s0 += 16) {
@@ -28,7 +28,8 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int dd) {
     for (int i = 0; i < 16; ++i)
       if (s0 + i < a.nseg) {
         p[(size_t)(s0 + i) * dd] = x;
-        x = decay_pow(g2, segment_tokens(s0 + i, a.seg_len, len)) * x + inc[i];
+        const int n = segment_tokens(s0 + i, a.seg_len, len);
+        x = (n == a.seg_len ? whole.of(x) : n > 0 ? end.of(x) : x) + inc[i];
       }
   }
 }

@@ -116,11 +116,11 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
   if (!STATE_ONLY && a.nseg > 1 && a.fold) {     // few segments: what those before this one add, instead of a launch that sums it up
     for (int j = 0; j < seg * a.pieces; ++j) {              // (four increments in flight at once: 40 registers spilled, 8 % slower)
       const float* inc = slots + (size_t)j * (D * D);
-      const float keep = decay_pow(g2, segment_tokens(j, a.piece_len, len));
+      const Fade fade(a.log_decay, h, segment_tokens(j, a.piece_len, len));
 #pragma unroll
       for (int it = 0; it < G::IT; ++it)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[it][r] = S[it][r] * keep + inc[at(it, r)];
+        for (int r = 0; r < 16; ++r) S[it][r] = fade.of(S[it][r]) + inc[at(it, r)];
     }
   }
 
@@ -144,7 +144,8 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
 #pragma unroll
     for (int j = 0; j < 8; ++j) fv[ks][j] = decay_pow(g2, 63 - (16 * ks + 8 * hi + j));
 
-  const float less64 = decay_pow_less_1(a.log_decay, h, C);
+  const Fade fade64(a.log_decay, h, C);
+  const int slow64 = __builtin_amdgcn_readfirstlane(fade64.slow);
   uint16_t* gout = const_cast<uint16_t*>(wo.p);
   auto store_rows = [&](int gi, const uint16_t* Ol) {
     const int tok0 = t_begin + gi * C;
@@ -234,10 +235,20 @@ __global__ __launch_bounds__(Cfg<D>::NT, 2) void decay_prefill_kernel(DecayArgs 
       for (int i = 0; i < 2 * G::IT; ++i) sop[i] = pack8(S[i / 2], 8 * (i % 2));
     }
     // ---- the state takes the group
-    float less = less64;
-    if (n < C) less = decay_pow_less_1(a.log_decay, h, n);
+    // (a branch of the whole workgroup: a select in every element costs twice as much, 2.7 % of the long prompts)
+    if (n < C) {
+      const Fade fade(a.log_decay, h, n);
 #pragma unroll
-    for (int it = 0; it < G::IT; ++it) S[it] += S[it] * less;
+      for (int it = 0; it < G::IT; ++it)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[it][r] = fade.of(S[it][r]);
+    } else if (slow64) {
+#pragma unroll
+      for (int it = 0; it < G::IT; ++it) S[it] += S[it] * fade64.f;
+    } else {
+#pragma unroll
+      for (int it = 0; it < G::IT; ++it) S[it] *= fade64.f;
+    }
     f32x16 away = {};
     O = f32x16{};
 #pragma unroll

@@ -70,11 +70,11 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
   if (!STATE_ONLY && a.nseg > 1 && a.fold) {
     for (int j = 0; j < seg * a.pieces; ++j) {
       const float* inc = slots + (size_t)j * (D * D);
-      const float keep = decay_pow(g2, segment_tokens(j, a.piece_len, len));
+      const Fade fade(a.log_decay, h, segment_tokens(j, a.piece_len, len));
 #pragma unroll
       for (int it = 0; it < G::RT; ++it)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[it][r] = S[it][r] * keep + inc[(32 * it + acc_row(r, hi)) * D + c0 + l32];
+        for (int r = 0; r < 16; ++r) S[it][r] = fade.of(S[it][r]) + inc[(32 * it + acc_row(r, hi)) * D + c0 + l32];
     }
   }
 
@@ -86,7 +86,8 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
     fv[r] = decay_pow(g2, C - 1 - acc_row(r, hi));
   }
   const float fq = decay_pow(g2, l32 + 1) * a.scale;
-  const float less32 = decay_pow_less_1(a.log_decay, h, C);
+  const Fade fade32(a.log_decay, h, C);
+  const int slow32 = __builtin_amdgcn_readfirstlane(fade32.slow);
 
   f32x4 rq[G::NP], rk[G::NP], rv[G::NP];
   auto request = [&](int tok0) {
@@ -158,10 +159,19 @@ __global__ __launch_bounds__(Cfg<D>::NT, 1) void decay_prefill_f32_kernel(DecayA
     float v[16];                            // V[acc_row(r)][c0 + l32]
 #pragma unroll
     for (int r = 0; r < 16; ++r) v[r] = Vl[acc_row(r, hi) * G::RS + c0 + l32];
-    float less = less32;
-    if (n < C) less = decay_pow_less_1(a.log_decay, h, n);
+    if (n < C) {
+      const Fade fade(a.log_decay, h, n);
 #pragma unroll
-    for (int it = 0; it < G::RT; ++it) S[it] += S[it] * less;
+      for (int it = 0; it < G::RT; ++it)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[it][r] = fade.of(S[it][r]);
+    } else if (slow32) {
+#pragma unroll
+      for (int it = 0; it < G::RT; ++it) S[it] += S[it] * fade32.f;
+    } else {
+#pragma unroll
+      for (int it = 0; it < G::RT; ++it) S[it] *= fade32.f;
+    }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int r = 0; r < 16; ++r)

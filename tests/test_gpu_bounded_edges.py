@@ -5,9 +5,11 @@ import pytest
 import torch
 
 from paper_2406_07368_amd import binding
+from plain_attention import decay_prefill, near
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
+NORM = {BF: None, F32: 5e-6}                     # as in test_gpu_decay.py
 
 
 def rows(B, H, L, d, dtype, seed, n=1):
@@ -189,3 +191,20 @@ def test_thousands_of_steps(dtype, kk, keep):
         steps = n if lam2 == 1 else min(n, 1 / (1 - lam2))
         rel = float((S[0, h].double() - want[0, h]).norm() / want[0, h].norm())
         assert rel <= 2 * 2.0 ** -24 / math.sqrt(3) * math.sqrt(steps) + 2.0 ** -22, (float(g[h]), rel)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("L", [160, 1000])
+def test_outliers_in_heads_that_forget_fast(dtype, L):
+    """The last token of a group is 1e6 (bf16: 1e8) times the others, of 160 tokens the square of that: what is left of it after the
+    next group is still right."""
+    g = torch.tensor([-0.05, -0.1, -0.16, -0.2, -0.25, -0.3, -0.4, -0.5, -0.6])
+    H, d = len(g), 64
+    q, k, v = rows(1, H, L, d, dtype, 56, 3)
+    for at in (63, L - 97):
+        v[:, :, at] *= 1e8 if dtype == BF else 1e6
+    want, S, size, A = decay_prefill(q.double(), k.double(), v.double(), g, 1.0)
+    out, Sg = binding.decay_prefill(*cuda(q, k, v, g), 1.0)
+    near(out, want, size, dtype, 2 if dtype == BF else 200, "out", NORM[dtype])
+    off = (Sg.double().cpu() - S).abs() - 2.0 ** -18 * A
+    assert float(off.max()) <= 0
