@@ -371,6 +371,7 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(WindowArgs a) {
           const int t = tw + acc_row(r, hi);
           if (!(window_sees(t, s, a.window, a.sinks) && t < len)) { x[r] = 0.f; y[r] = 0.f; }
         }
+        if (half == 0 && tw == 0 && hi == 0) y[0] = 0.f;   // (acc_row(0, 0) is 0: token 0 sees only itself, as in dq)
       }
     };
     weigh(0); weigh(1);

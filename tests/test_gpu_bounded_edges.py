@@ -208,3 +208,19 @@ def test_outliers_in_heads_that_forget_fast(dtype, L):
     near(out, want, size, dtype, 2 if dtype == BF else 200, "out", NORM[dtype])
     off = (Sg.double().cpu() - S).abs() - 2.0 ** -18 * A
     assert float(off.max()) <= 0
+
+
+@pytest.mark.parametrize("H,Hkv,d,W,sinks", [(4, 2, 64, 30, 2), (4, 1, 128, 500, 0), (2, 2, 128, 1, 1)])
+def test_gradient_of_a_sequence_of_one_token_in_a_batch(H, Hkv, d, W, sinks):
+    """Its softmax is over one key and constant: dq and dk are 0, as they are where the token comes alone."""
+    B, L = 3, 300
+    q, do = cuda(*rows(B, H, L, d, BF, 57, 2))
+    k, v = cuda(*rows(B, Hkv, L, d, BF, 58, 2))
+    lens = torch.tensor([1, L, 1], dtype=torch.int32, device="cuda")
+    out, lse, _ = binding.window_prefill(q, k, v, W, sinks, 3.0, lens, want_lse=True)
+    dq, dk, dv = binding.window_backward(q, k, v, out, lse, do, W, sinks, 3.0, lens)
+    for b in (0, 2):
+        one = [x[b:b + 1, :, :1].contiguous() for x in (q, k, v, out, do)]
+        gq, gk, gv = binding.window_backward(*one[:4], lse[b:b + 1, :, :1].contiguous(), one[4], W, sinks, 3.0)
+        assert not dq[b].any() and not dk[b].any() and not gq.any() and not gk.any()
+        assert torch.allclose(dv[b, :, :1].float(), gv[0].float(), rtol=2.0 ** -7, atol=0)     # (shares added up in another order: one step of bf16)
