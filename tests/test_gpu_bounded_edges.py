@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2406_07368_amd import binding
-from plain_attention import decay_prefill, near
+from plain_attention import decay_prefill, near, window_attend, window_seen
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -224,3 +224,28 @@ def test_gradient_of_a_sequence_of_one_token_in_a_batch(H, Hkv, d, W, sinks):
         gq, gk, gv = binding.window_backward(*one[:4], lse[b:b + 1, :, :1].contiguous(), one[4], W, sinks, 3.0)
         assert not dq[b].any() and not dk[b].any() and not gq.any() and not gk.any()
         assert torch.allclose(dv[b, :, :1].float(), gv[0].float(), rtol=2.0 ** -7, atol=0)     # (shares added up in another order: one step of bf16)
+
+
+@pytest.mark.parametrize("B,H,Hkv,L,d,W,sinks,ragged", [
+    (2, 2, 1, 1, 128, 5, 3, False), (1, 2, 2, 31, 128, 7, 0, False), (2, 4, 2, 65, 128, 1, 0, True), (1, 2, 1, 129, 64, 1, 64, False),
+    (2, 2, 1, 300, 64, 5, 2, True), (1, 4, 2, 200, 128, 2, 0, False), (2, 24, 3, 85, 128, 8, 1, True)])
+def test_gradient_of_narrow_windows_in_the_norm(B, H, Hkv, L, d, W, sinks, ragged):
+    """dq and dk of windows of 8 tokens and fewer, exactly 0 where every token sees only itself."""
+    q, do = rows(B, H, L, d, BF, 59, 2)
+    k, v = rows(B, Hkv, L, d, BF, 60, 2)
+    lens = torch.tensor([L, L // 2 + 1][:B], dtype=torch.int32) if ragged else None
+    live = torch.ones((B, 1, L, 1), dtype=torch.bool) if lens is None else (torch.arange(L) < lens[:, None])[:, None, :, None]
+    x = [t.double().requires_grad_() for t in (q, k, v)]
+    G = H // Hkv
+    Q, K, V = (torch.where(live, t, 0.0) for t in x)
+    t = torch.arange(L)
+    out = window_attend(Q, K, V, window_seen(t[None], t[:, None], W, sinks), 0.2)[0]
+    want = torch.autograd.grad(torch.where(live, out, 0.0), x, do.double())
+    a = cuda(q, k, v, do, lens)
+    o, lse, _ = binding.window_prefill(*a[:3], W, sinks, 0.2, a[4], want_lse=True)
+    for n, g, w in zip("qkv", binding.window_backward(*a[:3], o, lse, a[3], W, sinks, 0.2, a[4]), want):
+        if n != "v" and (L == 1 or W == 1 and sinks == 0):
+            assert not g.any()
+            continue
+        # two independent roundings to bf16, dS (or P) and the result, each 2^-8 / sqrt(3) at most in the mean square
+        assert float((g.double().cpu() - w).norm()) <= math.sqrt(2 / 3) * 2.0 ** -8 * float(w.norm()), n
