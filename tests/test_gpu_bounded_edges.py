@@ -249,3 +249,18 @@ def test_gradient_of_narrow_windows_in_the_norm(B, H, Hkv, L, d, W, sinks, ragge
             continue
         # two independent roundings to bf16, dS (or P) and the result, each 2^-8 / sqrt(3) at most in the mean square
         assert float((g.double().cpu() - w).norm()) <= math.sqrt(2 / 3) * 2.0 ** -8 * float(w.norm()), n
+
+
+@pytest.mark.parametrize("B,H,Hkv,d,kk,W,sinks,pos", STEPS)
+def test_steps_of_bf16_rows_are_off_by_their_own_rounding(B, H, Hkv, d, kk, W, sinks, pos):
+    q, k, v, kc, vc, P = step_case(BF, B, H, Hkv, d, kk, W, sinks, pos)
+    a = cuda(q, k, v, kc, vc, P)
+    got = binding.window_step(*a[:3], tuple(a[3:]), W, sinks, 0.2).double().cpu()
+    held = torch.tensor([s if s < sinks else sinks + (s - sinks) % W for s in range(pos) if s < sinks or s >= pos - W])
+    at = torch.tensor([s for s in range(pos) if s < sinks or s >= pos - W])
+    K, V = (torch.cat([x[:, :, held], y], 2).double() for x, y in ((kc, k), (vc, v)))
+    new = pos + torch.arange(kk)
+    want, _, size = window_attend(q.double(), K, V, window_seen(torch.cat([at, new])[None], new[:, None], W, sinks), 0.2)
+    # a weight is off by 2^-8 of its second term, which is 2^-8 of it at most; fp32 sums as in plain_attention.near
+    assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -16 + 2.0 ** -18) * size).all())
+    assert float((got - want).norm()) <= float((want.to(BF).double() - want).norm()) + 2.0 ** -16 * float(size.norm())
