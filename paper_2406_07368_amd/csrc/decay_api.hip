@@ -12,18 +12,23 @@ using namespace linattn;
 namespace {
 
 // The state before every segment from what the segments add to it: S_{s+1} = lambda^{tokens of s} S_s + inc_s.  A thread
-// owns one element, so that every request is a whole row; the increments of sixteen segments are requested at a time.
+// owns one element, so that every request is a whole row; the increments of sixteen segments are requested at a time, the first
+// ahead of the factors (6.2 -> 4.7 us at 8 heads of 128 over 1000 tokens).
 __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int dd) {
   const int per = dd / 256, bhr = blockIdx.x / per, e = blockIdx.x % per * 256 + threadIdx.x;
   const int bh = bhr / a.roles, b = bh / a.H;
   const int len = clamp_len(a.lens, b, a.L);
-  const Fade whole(a.log_decay, bh % a.H, a.seg_len), end(a.log_decay, bh % a.H, len % a.seg_len);   // (over a segment; over the one that the sequence ends in)
   float* p = a.ws + (size_t)bhr * a.nseg * dd + e;
   float x = a.S_in ? a.S_in[(size_t)bh * dd + e] : 0.f;
-  for (int s0 = 0; s0 < a.nseg; s0 += 16) {
-    float inc[16];
+  float inc[16];
+  auto request = [&](int s0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) inc[i] = s0 + i < a.nseg - 1 ? p[(size_t)(s0 + i) * dd] : 0.f;
+  };
+  request(0);
+  const Fade whole(a.log_decay, bh % a.H, a.seg_len), end(a.log_decay, bh % a.H, len % a.seg_len);   // (over a segment; over the one that the sequence ends in)
+  for (int s0 = 0; s0 < a.nseg; s0 += 16) {
+    if (s0 > 0) request(s0);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (s0 + i < a.nseg) {
