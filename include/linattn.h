@@ -416,8 +416,9 @@ linattn_status linattn_decay_step(const linattn_decay_desc *desc, int32_t kk,
  *
  *   out_t = sum_s softmax_s(scale * q_t.k_s) v_s,   lse_t = log sum_s exp(scale * q_t.k_s)
  *
+ * Scores are fp32 numbers, and the exponent of a weight carries their rounding: |scale * q_t.k_s| is to stay below 2^30.
  * A non-finite value in a key or value row of a sequence may also reach rows of the same sequence that do not see
- * it (never those of another sequence). */
+ * it (never those of another sequence).  A NaN in q or in a visible key and a score of +inf make NaN of the output row. */
 typedef struct {
   int32_t B, H, H_kv;      /* batch rows, query heads, key/value heads (a divisor of H); B * H <= 2^20 */
   int32_t d;               /* head dimension: 64 or 128                                */
@@ -432,6 +433,8 @@ typedef struct {
 #define LINATTN_MAX_SINKS 64
 
 /* All L tokens of every (b, h), from the start of the sequences: 0 <= L <= 2^30, B * H * ceil(L / 128) <= 2^23.
+ * bf16 rows: matrix cores, fp32 accumulation and statistics; the weights are rounded to bf16 once for their product with v.
+ * fp32 rows: exact fp32 products.
  *   q [B,H,L,d], k, v [B,H_kv,L,d], out [B,H,L,d]  by strides
  *   lse          out, optional  float [B,H,L] dense; -inf behind a sequence's end
  *   kcache, vcache  out, optional (all three or none)  [B,H_kv,sinks+window,d] dense, i/o dtype: the rows that later
@@ -462,7 +465,8 @@ linattn_status linattn_window_backward(const linattn_window_desc *desc, int32_t 
  *                advanced by one owner; a negative count is read as 0, and pos + kk must stay below 2^31.
  *   n_commit     in, optional  device int32 [B], clamped into 0..kk: the first n_commit[b] tokens enter the cache
  *                (NULL: all; 0: nothing changes).  All kk outputs are produced.
- *   workspace    linattn_window_step_workspace_bytes(desc, kk) bytes (may be 0); used by one call at a time */
+ *   workspace    linattn_window_step_workspace_bytes(desc, kk) bytes (may be 0); used by one call at a time
+ * bf16 rows: the weights carry sixteen significant bits into their product with v.  fp32 rows: exact fp32 products. */
 size_t linattn_window_step_workspace_bytes(const linattn_window_desc *desc, int32_t kk);
 linattn_status linattn_window_step(const linattn_window_desc *desc, int32_t kk,
                                    const void *q, const void *k, const void *v,

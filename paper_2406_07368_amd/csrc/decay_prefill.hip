@@ -17,12 +17,15 @@
 // V' enters the state as the sum of TERMS bf16 terms.  Two carry sixteen significant bits: with one, the gradient's error was
 // 1.65 times that of the final rounding alone, with two it is 1.4 times.  A state that is handed back in fp32 takes three, all
 // of an fp32 product's bits (its error at LLaMA size: 3.6e-7, with two terms 2.5e-6, for 264 us in the place of 240).
+// The weights P and, for its read-out, the state are rounded to bf16 once: the outputs are off by 2.34e-3 in the 2-norm, of which their
+// own rounding is 1.66e-3.  The read-out in two terms: 1.79e-3, for 12 % more time (275 -> 306 us, the gradient of the training
+// batch 315 -> 364), which these kernels, bound by the issue of instructions, do not have.
 //
 // The gradient is the same function with other roles: dq = F(dout, v, k), and over reversed time dk = F(v, dout, q),
 // dv = F(k, q, dout); a launch carries up to three roles.
 //
 // HBM is the floor (8 d bytes a token and head: at d = 128 1 KB, against 82 K flops), and what bounds it now is the issue of vector
-// and matrix instructions at the clock that the power limit leaves (2.0 GHz).  Measured at 256 heads of 128 over 4096 tokens: 240 us with
+// and matrix instructions at the clock that the power limit leaves (2.0 GHz).  Measured at 256 heads of 128 over 4096 tokens: 236 us with
 // two terms, 264 with three (1.07 GB of rows: 4.5 and 4.1 TB/s; a copy runs at 5.1).
 #include "common.h"
 #include "decay.h"

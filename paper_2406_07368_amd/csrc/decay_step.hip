@@ -8,7 +8,7 @@
 // columns of S in registers -- requested before anything else --, every draft's read-out is a sum over a thread's rows,
 // the lanes of a wave that share columns, and the four waves; the same registers then take the kept drafts and go back.
 // The products of the drafts among themselves (at most 136) are made by every workgroup of a head again: they cost
-// less than a launch of their own or a wider workgroup's wait.  Measured: four drafts on 1024 heads of 128 25 us, 5.4 TB/s (32
+// less than a launch of their own or a wider workgroup's wait.  Measured: four drafts on 1024 heads of 128 26 us, 5.3 TB/s (32
 // columns a workgroup: a 128-byte line per row; 4096 workgroups of 16 KB).
 #include "common.h"
 #include "decay.h"

@@ -15,8 +15,13 @@
 // query tiles that see nothing of it but sinks are shared out over workgroups of their own, and where there are few key
 // tiles each is shared by several workgroups.  Their sums (fp32) go to the workspace and are added up in a fixed order.
 //
-// Bound: LDS reads and vector ALUs beside the matrix cores (14 d flops a visible pair here).  Measured at 64 heads of 128 over sequences of
-// up to 4096 tokens, a window of 1024: dq 183 us, 840 TFLOP/s; dk and dv 321 us, 650 TFLOP/s.
+// P and dS are rounded to bf16 once for the products, whose sums are fp32: the gradients are off by 2.35e-3 in the 2-norm, of which their
+// own rounding is 1.66e-3.  In two terms each 1.67e-3, for dq 185 -> 225 us, dk and dv 300 -> 411.
+//
+// Bound (14 d flops a visible pair here): no unit alone.  dq: matrix cores 48 % of the cycles, vector ALUs 35, LDS 26; dk and dv: 38, 28 and
+// 29 -- two waves on a SIMD, whose accumulators leave registers for operands one step ahead, wait for each other's units in turn.
+// Measured at 64 heads of 128 over sequences of up to 4096 tokens, a window of 1024: dq 183 us, 840 TFLOP/s; dk and dv 300 to 321 us
+// (boards differ), 650 TFLOP/s.
 #include "common.h"
 #include "kernels.h"
 #include "mfma_util.h"

@@ -9,8 +9,11 @@
 // accumulator layout is the operand layout up to a permutation of the keys, which is applied to the transposed reads of
 // V.  Key tiles that no query of the tile sees are not visited; masks are computed only where a border crosses.
 //
-// Bound: the vector ALUs (some 190 instructions for 32 products of a wave, 32 of them exponentials; 55 % of the cycles) beside the matrix
-// cores (4 d flops a visible pair; 52 %), at 1.8 GHz (power).  Measured at 64 heads of 128 over 8192 tokens, a window of 2048: 505 to 525 us
+// The weights are rounded to bf16 once for their product with V (not in the sum that divides it): out is off by 2.2e-3 in the 2-norm, of
+// which its own rounding is 1.6e-3.  In two terms the first part goes, for a third more time (530 -> 700 us at the size below).
+//
+// Bound: the matrix cores (4 d flops a visible pair; 53 % of the cycles) beside the vector ALUs (some 190 instructions for 32 products
+// of a wave, 32 of them exponentials; 49 %), at 1.8 GHz (power).  Measured at 64 heads of 128 over 8192 tokens, a window of 2048: 505 to 525 us
 // (boards differ), 940 TFLOP/s of 1361 that a large library product reaches.
 #include "common.h"
 #include "kernels.h"

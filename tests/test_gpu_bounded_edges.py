@@ -66,6 +66,29 @@ def test_step_hands_on_what_is_not_finite(dtype, B, H, Hkv, d, kk, W, sinks, pos
         assert bool(torch.isfinite(got.cpu()[~hit]).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("where", ["query", "infinite score", "key"])
+def test_prompt_hands_on_what_is_not_finite(dtype, where):
+    B, H, Hkv, L, d, W, sinks = 2, 4, 2, 300, 128, 100, 3
+    q, = rows(B, H, L, d, dtype, 55)
+    k, v = rows(B, Hkv, L, d, dtype, 65, 2)
+    hit, t = torch.zeros((B, H, L), dtype=torch.bool), 150
+    if where == "query":
+        q[0, 1, t, 3] = math.nan
+        hit[0, 1, t] = True
+    elif where == "infinite score":
+        q[0, 0, t + 20], k[0, 0, t] = 1e30, 1e30
+        hit[0, 0, t + 20] = True
+    else:
+        k[0, 0, t, 5] = math.nan
+        hit[0, :H // Hkv, t:t + W] = True
+    out, lse, _ = binding.window_prefill(*cuda(q, k, v), W, sinks, 0.2, want_lse=True)
+    assert bool(torch.isnan(out.cpu()[hit]).all()) and bool(torch.isnan(lse.cpu()[hit]).all())
+    if where == "query":
+        assert bool(torch.isfinite(out.cpu()[~hit]).all())
+    assert bool(torch.isfinite(out[1]).all()) and bool(torch.isfinite(out[:, H // Hkv:]).all())
+
+
 def keep_busy():
     """Some 50 ms of work on the current stream."""
     x = torch.ones((8192, 8192), dtype=BF, device="cuda")
