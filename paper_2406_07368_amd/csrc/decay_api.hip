@@ -57,6 +57,8 @@ struct Plan {
 // one more read of K and V, if what that saves -- of `groups` steps all but 1/n, and half as many steps of the first pass -- makes up
 // for the second launch: some four steps of bf16 (d = 128, 120 walks in two segments: 44 us of 47 at 16 groups, but 30 of 27 at 8),
 // half a one of fp32.
+// Where more than half of the chip is busy none is cut: segments of more walks than have room run in two rounds (d = 128, bf16, 130 walks
+// of 4096 tokens: whole 208 us, in two 286, in three 240; 250 walks: 263, 351, 378; fp32 943, 1169, 947 and 963, 1197, 1291).
 Plan plan(const linattn_decay_desc* d, int32_t L, int roles) {
   Plan p{1, L, 1, 0};
   const bool f32 = d->io_dtype == LINATTN_F32;

@@ -171,6 +171,27 @@ def test_memory_of_calls_on_a_stream():
             del spoilt, got
 
 
+def test_calls_on_a_stream_in_a_graph():
+    """The capturing stream named in the call: the replays give the eager bits, with other work between."""
+    x, calls = calls_for_a_stream()
+    calls = [calls[i] for i in (0, 1, 3, 4, 5, 7, 8)]                   # (those that change nothing that they are given)
+    want = [[y.clone() for y in f(x, None)] for f in calls]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            held = [f(x, side) for f in calls] + [f(x, side.cuda_stream) for f in calls]
+    for i in range(4):
+        for y in (z for h in held for z in h):
+            y.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (h, w) in enumerate(zip(held, want + want)):
+            assert all(torch.equal(a, b) for a, b in zip(h, w)), i
+        [f(x, None) for f in calls]
+
+
 def test_memory_that_the_current_stream_still_uses():
     """A call on an idle stream, while the current stream is behind and will still write to memory that was let go."""
     x, calls = calls_for_a_stream()
